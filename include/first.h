@@ -336,6 +336,100 @@ int first_op_gemm_nt(void *hip_stream, int32_t dtype, const void *A, const void 
 int first_op_gemm_nt_f32a(void *hip_stream, const float *A, const void *W, float *C, int32_t m,
                           int32_t n, int32_t k, int32_t accumulate);
 
+/* ---- operators of a step over drafted tokens ---------------------------------------------
+ *
+ * What a program needs to verify trees of drafted tokens of several tasks' requests at once: projections with an adapter per row,
+ * rotary positions, attention over the paged cache and the tree, and the draw.  They hold no state: every buffer is the caller's,
+ * a workspace is written before it is read, and it is free again when the call's last kernel has ended - calls that may run at the same time
+ * (other streams, graphs that are replayed side by side) need workspaces of their own.  All of them can be captured into a graph.  Kernels go to
+ * hip_stream, whose device must be the current one.  FIRST_ERR_ARG: what the text says; FIRST_ERR_CAPACITY: a workspace that is too small, or a
+ * size beyond a stated limit; nothing is enqueued on error, and the text is first_last_error(NULL).  Sizes of zero are no error: nothing is
+ * enqueued.  The *_workspace functions return bytes, or a negative error code. */
+
+/* C[i] (+)= W A[i] + scale[a] Lb[a] (La[a] A[i]),  a = adapter[i] the adapter of row i: first_op_gemm_nt with the adapters of many
+ * tasks (Section 4.2) beside one shared matrix, instead of one task's merged into it.  An adapter outside [0, n_adapters) is none: the
+ * row is the shared projection alone.
+ *   A DEV [m, k], W DEV [n, k], La DEV [n_adapters, r, k], Lb DEV [n_adapters, n, r] of dtype, on 16 bytes; adapter DEV int32 [m];
+ *   scale DEV fp32 [n_adapters] (lora_alpha / r); C DEV fp32 [m, n], which none of the others may overlap; k multiple of 8; 1 <= r <= 64.
+ *   m <= 2^20.  Adapters of smaller ranks: zeros in the rest of La or Lb.
+ * Products of bf16 values are exact, all sums fp32; La A[i] stays in fp32 (bf16: three bf16 parts, which is all of it). */
+int64_t first_op_gemm_nt_lora_workspace(int32_t dtype, int32_t m, int32_t n, int32_t k, int32_t r);
+int first_op_gemm_nt_lora(void *hip_stream, int32_t dtype, const void *A, const void *W, const void *La, const void *Lb,
+                          const int32_t *adapter, const float *scale, float *C, int32_t m, int32_t n, int32_t k, int32_t n_adapters,
+                          int32_t r, int32_t accumulate, void *workspace, int64_t workspace_bytes);
+
+#define FIRST_ROPE_HALF        0   /* pair i of a head: elements i and i + rot_dim / 2 (the layout of the models here) */
+#define FIRST_ROPE_INTERLEAVED 1   /* pair i: elements 2 i and 2 i + 1 */
+#define FIRST_ROPE_NONE   0        /* f_i = base^(-2 i / rot_dim)                                                    */
+#define FIRST_ROPE_LINEAR 1        /* f_i / factor: positions squeezed into the original context                     */
+#define FIRST_ROPE_BANDS  2        /* by how often a pair turns within the original context, t = original_len f_i / (2 pi): f_i for t >= high,
+                                      f_i / factor for t <= low, between them a blend, linear in t                     */
+typedef struct first_rope_desc {
+  int32_t dtype;                   /* of x and y                                                                     */
+  int32_t n_heads, head_dim;       /* head_dim <= 256                                                                */
+  int32_t rot_dim;                 /* even, 2 .. head_dim: the first rot_dim elements of a head turn, the rest pass  */
+  int32_t layout, scaling;         /* FIRST_ROPE_*                                                                   */
+  int32_t inverse;                 /* 1: turn by -angle; of a gradient this is the transpose, the backward pass      */
+  int32_t original_len;            /* FIRST_ROPE_BANDS                                                               */
+  float base, factor;              /* factor: LINEAR and BANDS                                                       */
+  float low, high;                 /* BANDS: low < high                                                              */
+  float amplitude;                 /* the turned elements are multiplied by it (1: plain rotation)                   */
+} first_rope_desc;
+/* Rotary positions: pair i of every head of row j is turned by positions[j] * f_i.  Rows of x and y are x_pitch and y_pitch elements apart
+ * (at least n_heads * head_dim), so that the heads of a packed projection output can be turned where they are.  y may be x; other overlaps
+ * are refused, but for row-by-row neighbours (same pitch, no element in common).  Angles are formed in fp64, one rounding to dtype at the end.
+ *   x, y DEV of dtype; positions DEV int32 [rows], any value. */
+int first_op_rope(void *hip_stream, const first_rope_desc *desc, const void *x, int64_t x_pitch, void *y, int64_t y_pitch,
+                  const int32_t *positions, int32_t rows);
+
+typedef struct first_tree_attn_desc {
+  int32_t dtype;                   /* of q, k, v, the cache and out                                                  */
+  int32_t n_q_heads, n_kv_heads;   /* query head h reads KV head h / (n_q_heads / n_kv_heads)                        */
+  int32_t head_dim;                /* 64 or 128                                                                      */
+  int32_t page_tokens;             /* 16                                                                             */
+  int32_t n_pages;                 /* pages of kv_layer                                                              */
+  int32_t max_pages;               /* entries of a sequence's row of the page table                                  */
+  int32_t mask_words;              /* 64-bit words of a node's mask                                                  */
+  float scale;                     /* of the scores, 1 / sqrt(head_dim) in the models here                           */
+} first_tree_attn_desc;
+/* Attention of drafted tokens.  Sequence b has nodes node_offsets[b] .. node_offsets[b + 1] - 1 (its drafted tokens, already rotated at their own
+ * positions) and lens[b] positions in the cache.  A node sees all of those and the nodes j of its sequence whose bit j of its mask is set (itself is
+ * one of them if it is to be); without a mask the nodes are a chain, node i sees 0 .. i.  out = softmax(scale q K^T) V over what it sees, lse the
+ * natural logarithm of the sum of exponentials; a node that sees nothing has out 0, lse -inf.  One node a sequence is an ordinary decode step.
+ *   q, out       DEV [N, n_q_heads, head_dim] of dtype;  k_new, v_new DEV [N, n_kv_heads, head_dim]: keys and values of the nodes
+ *   kv_layer     DEV one layer's pages, [page][K|V][n_kv_heads][16][head_dim] as in the contexts here.  May be NULL if max_len or max_pages is 0
+ *   page_table   DEV int32 [B, max_pages]; a page outside [0, n_pages) holds nothing: its positions are not seen
+ *   lens         DEV int32 [B], taken as at most max_len and 16 max_pages, and as 0 below it.  Cached positions >= lens[b] are never used, whatever
+ *                they hold, nor is what stands in k_new / v_new at nodes that a node does not see, infinities and NaN included
+ *   node_offsets DEV int32 [B + 1], ascending; of a sequence's nodes the first max_nodes are computed, rows of other nodes stay as they are
+ *   tree_mask    DEV uint64 [N, mask_words], mask_words * 64 >= max_nodes (may be NULL)
+ *   lse          DEV fp32 [N, n_q_heads] (may be NULL)
+ * N = node_offsets[B], max_nodes and max_len are bounds that the host knows; out must overlap nothing else. */
+int64_t first_op_tree_attn_workspace(const first_tree_attn_desc *desc, int32_t B, int32_t N, int32_t max_nodes, int32_t max_len);
+int first_op_tree_attn(void *hip_stream, const first_tree_attn_desc *desc, const void *q, const void *k_new, const void *v_new,
+                       const void *kv_layer, const int32_t *page_table, const int32_t *lens, const int32_t *node_offsets,
+                       const uint64_t *tree_mask, void *out, float *lse, int32_t B, int32_t N, int32_t max_nodes, int32_t max_len,
+                       void *workspace, int64_t workspace_bytes);
+
+/* Tokens drawn from rows of logits, each row by rules of its own; the draws are the caller's, as in first_sample_top_k.  The tokens of
+ * a row stand in order of their logits, largest first, equal ones by index; a token weighs w = exp((l - l_max) / temperature).  Each rule keeps a prefix
+ * of that order and the shortest is kept:
+ *   top_k        the first top_k tokens                                                     (off: <= 0, or NULL)
+ *   top_p        of those, the tokens before which less than top_p of their mass lies       (off: >= 1, NaN, or NULL); the first token always stays
+ *   min_p        tokens with w >= min_p                                                     (off: <= 0, NaN, or NULL); the first token always stays
+ * and the token is the first whose cumulative weight exceeds uniforms * (sum of the kept weights).  A temperature of 0 or less (or NaN)
+ * takes the first token of the order.  Logits that are NaN or -inf, and weights that are 0 in 64 bits, are no tokens; if the largest logit is +inf, the
+ * tokens with +inf share the draw.  A row without tokens: token -1, logprob -inf, kept 0.  Weights in fp64, their sums exact to 2^-45 of the largest
+ * weight a token (2^18 tokens), whatever the order of additions: results do not depend on the launch.
+ *   logits      DEV fp32 [rows], pitch elements apart;  uniforms DEV fp32 [rows], in [0, 1) (others are taken as the nearest)
+ *   temperature DEV fp32 [rows] (NULL: 1);  top_k DEV int32 [rows];  top_p, min_p DEV fp32 [rows]
+ *   token_out   DEV int32 [rows];  logprob_out DEV fp32 [rows] logarithm of the token's share of the kept weights (may be NULL)
+ *   kept_out    DEV int32 [rows] number of tokens kept (may be NULL) */
+int64_t first_sample_workspace(int32_t rows, int32_t vocab);
+int first_sample(void *hip_stream, const float *logits, int64_t pitch, int32_t rows, int32_t vocab, const float *uniforms,
+                 const float *temperature, const int32_t *top_k, const float *top_p, const float *min_p, int32_t *token_out,
+                 float *logprob_out, int32_t *kept_out, void *workspace, int64_t workspace_bytes);
+
 /* Per-phase timestamps of the last persistent-kernel decode step (FIRST_OPT_STEP_TIMING = 1),
  * taken by workgroup 0 on the 100 MHz device clock: for each phase (QKV, O, gate/up, down of
  * every kept layer in order, then the LM head) twelve values: phase begins (twice), attention

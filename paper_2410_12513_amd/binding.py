@@ -16,7 +16,11 @@ EXPORTS = ["first_create", "first_destroy", "first_prefill_route", "first_set_ma
            "first_decode_step", "first_set_option", "first_sync", "first_last_error", "first_seq_len",
            "first_batch", "first_kv_read", "first_kv_write", "first_get_hidden", "first_set_page_order", "first_sample_top_k",
            "first_num_pages", "first_op_gemv", "first_op_gemm_nt", "first_op_gateup", "first_step_timing", "first_op_gemm_nt_f32a", "first_set_seq_len", "first_kv_usage", "first_soft_forward",
-           "first_lora_merge", "first_sample_top_k_static", "first_decode_step_sampled"]
+           "first_lora_merge", "first_sample_top_k_static", "first_decode_step_sampled",
+           "first_op_gemm_nt_lora", "first_op_gemm_nt_lora_workspace", "first_op_rope", "first_op_tree_attn",
+           "first_op_tree_attn_workspace", "first_sample", "first_sample_workspace"]
+ROPE_LAYOUTS = {"half": 0, "interleaved": 1}
+ROPE_SCALINGS = {"none": 0, "linear": 1, "bands": 2}
 
 
 class FirstError(RuntimeError):
@@ -41,6 +45,16 @@ class _Weights(C.Structure):
                 ("w_up", C.POINTER(C.c_void_p)), ("w_down", C.POINTER(C.c_void_p)), ("router", C.c_void_p)]
 
 
+class _RopeDesc(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("dtype", "n_heads", "head_dim", "rot_dim", "layout", "scaling", "inverse", "original_len")] + \
+               [(n, C.c_float) for n in ("base", "factor", "low", "high", "amplitude")]
+
+
+class _TreeAttnDesc(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("dtype", "n_q_heads", "n_kv_heads", "head_dim", "page_tokens", "n_pages", "max_pages", "mask_words")] + \
+               [("scale", C.c_float)]
+
+
 def lib_path() -> str:
     return os.path.join(HERE, "libfirst.so")
 
@@ -62,6 +76,14 @@ def load_library():
         for name in EXPORTS:
             if name != "first_last_error":
                 getattr(lib, name).restype = C.c_int
+        p, i, l = C.c_void_p, C.c_int32, C.c_int64
+        for name, args in (("first_op_gemm_nt_lora", (p, i, p, p, p, p, p, p, p, i, i, i, i, i, i, p, l)),
+                           ("first_op_gemm_nt_lora_workspace", (i,) * 5), ("first_op_rope", (p, p, p, l, p, l, p, i)),
+                           ("first_op_tree_attn", (p,) * 12 + (i,) * 4 + (p, l)), ("first_op_tree_attn_workspace", (p,) + (i,) * 4),
+                           ("first_sample", (p, p, l, i, i) + (p,) * 8 + (p, l)), ("first_sample_workspace", (i, i))):
+            getattr(lib, name).argtypes = args
+            if name.endswith("_workspace"):
+                getattr(lib, name).restype = l
         _LIB = lib
     return _LIB
 
@@ -345,3 +367,166 @@ def sample_top_k_static(logits: torch.Tensor, uniforms: torch.Tensor, temperatur
                                        C.c_float(temperature), C.c_int32(top_k), _ptr(token_out), _ptr(candidates_out))
     if rc != 0:
         raise FirstError(rc, lib.first_last_error(None).decode())
+
+
+# ---- operators of a step over drafted tokens (stateless; stream=None: the current stream of the tensors' device) --------------
+
+
+class _On:
+    """The device of `t` current, and the stream to launch on: that of `stream`, or the device's current one."""
+
+    def __init__(self, t: torch.Tensor, stream):
+        if not t.is_cuda:
+            raise ValueError("expected device tensors")
+        self.guard = torch.cuda.device(t.device)
+        self.stream, self.device = stream, t.device
+
+    def __enter__(self):
+        self.guard.__enter__()
+        if self.stream is None:
+            self.stream = torch.cuda.current_stream(self.device)
+        return self.stream.cuda_stream
+
+    def __exit__(self, *exc):
+        return self.guard.__exit__(*exc)
+
+    def workspace(self, given: Optional[torch.Tensor], need: int):
+        """(address, bytes) of the caller's workspace, or of one that lives until the stream is through with it."""
+        if need < 0:
+            _raise(need)
+        if given is None:
+            if need == 0:
+                return 0, 0
+            given = torch.empty(need, dtype=torch.uint8, device=self.device)
+            given.record_stream(self.stream)
+        elif given.device != self.device or not given.is_contiguous():
+            raise ValueError("workspace: expected a contiguous tensor on the device of the others")
+        return given.data_ptr(), given.numel() * given.element_size()
+
+
+def _raise(rc: int) -> None:
+    raise FirstError(int(rc), load_library().first_last_error(None).decode())
+
+
+def _same(t: torch.Tensor, dtype: torch.dtype, shape, like: torch.Tensor, name: str) -> int:
+    if t.dtype != dtype or t.device != like.device or not t.is_contiguous() or t.shape != shape:
+        raise ValueError(f"{name}: expected a contiguous tensor of {dtype}, {list(shape)}, on {like.device}")
+    return t.data_ptr()
+
+
+def _code(t: torch.Tensor, name: str) -> int:
+    if t.dtype not in (torch.bfloat16, torch.float32):
+        raise ValueError(f"{name}: expected bfloat16 or float32")
+    return DTYPE_CODES["bf16" if t.dtype == torch.bfloat16 else "fp32"]
+
+
+def op_gemm_nt_lora_workspace(A: torch.Tensor, W: torch.Tensor, La: torch.Tensor) -> int:
+    """Bytes of workspace that op_gemm_nt_lora needs for these shapes."""
+    n = load_library().first_op_gemm_nt_lora_workspace(_code(W, "W"), A.shape[0], W.shape[0], W.shape[1], La.shape[1])
+    return n if n >= 0 else _raise(n)
+
+
+def op_gemm_nt_lora(A: torch.Tensor, W: torch.Tensor, La: torch.Tensor, Lb: torch.Tensor, adapter: torch.Tensor, scale: torch.Tensor, Cm: torch.Tensor,
+                    accumulate: bool = False, workspace: Optional[torch.Tensor] = None, stream=None) -> None:
+    """Cm[i] (+)= W A[i] + scale[a] Lb[a] (La[a] A[i]), a = adapter[i] (outside [0, adapters): none).  A [m, k], W [n, k], La [adapters, r, k],
+    Lb [adapters, n, r] of one type; Cm fp32 [m, n]."""
+    lib = load_library()
+    code = _code(W, "W")
+    m, k = A.shape
+    n, (ads, r) = W.shape[0], La.shape[:2]
+    ptrs = [_same(A, W.dtype, (m, k), W, "A"), _same(W, W.dtype, (n, k), W, "W"), _same(La, W.dtype, (ads, r, k), W, "La"),
+            _same(Lb, W.dtype, (ads, n, r), W, "Lb"), _same(adapter, torch.int32, (m,), W, "adapter"), _same(scale, torch.float32, (ads,), W, "scale"),
+            _same(Cm, torch.float32, (m, n), W, "C")]
+    on = _On(W, stream)
+    with on as st:
+        ws, size = on.workspace(workspace, lib.first_op_gemm_nt_lora_workspace(code, m, n, k, r))
+        rc = lib.first_op_gemm_nt_lora(st, code, *ptrs, m, n, k, ads, r, int(accumulate), ws, size)
+    if rc != 0:
+        _raise(rc)
+
+
+def op_rope(x: torch.Tensor, positions: torch.Tensor, y: torch.Tensor, rot_dim: Optional[int] = None, layout: str = "half", base: float = 10000.0,
+            scaling: str = "none", factor: float = 1.0, low: float = 1.0, high: float = 4.0, original_len: int = 8192, amplitude: float = 1.0,
+            inverse: bool = False, stream=None) -> None:
+    """Rotary positions of the heads of x [rows, heads, head_dim] into y (which may be x).  The rows may be strided: heads of a packed projection
+    output.  inverse: turn back, which on a gradient is the backward pass."""
+    lib = load_library()
+    code = _code(x, "x")
+    rows, heads, hd = x.shape
+    for t, name in ((x, "x"), (y, "y")):
+        if t.dtype != x.dtype or t.device != x.device or t.shape != x.shape or (t.numel() > 0 and (t.stride(2) != 1 or (heads > 1 and t.stride(1) != hd))):
+            raise ValueError(f"{name}: expected [rows, heads, head_dim] of one type on one device, the heads of a row one after the other")
+    if layout not in ROPE_LAYOUTS or scaling not in ROPE_SCALINGS:
+        raise ValueError(f"layout is one of {list(ROPE_LAYOUTS)}, scaling one of {list(ROPE_SCALINGS)}")
+    pos = _same(positions, torch.int32, (rows,), x, "positions")
+    d = _RopeDesc(code, heads, hd, hd if rot_dim is None else rot_dim, ROPE_LAYOUTS[layout], ROPE_SCALINGS[scaling], int(inverse), original_len, base, factor,
+                  low, high, amplitude)
+    pitch = lambda t: t.stride(0) if rows > 1 else heads * hd  # noqa: E731
+    with _On(x, stream) as st:
+        rc = lib.first_op_rope(st, C.byref(d), x.data_ptr(), pitch(x), y.data_ptr(), pitch(y), pos, rows)
+    if rc != 0:
+        _raise(rc)
+
+
+def _tree_desc(q: torch.Tensor, k_new: torch.Tensor, pages: int, max_pages: int, words: int, scale: Optional[float]) -> _TreeAttnDesc:
+    hd = q.shape[2]
+    return _TreeAttnDesc(_code(q, "q"), q.shape[1], k_new.shape[1], hd, 16, pages, max_pages, words, hd ** -0.5 if scale is None else scale)
+
+
+def op_tree_attn_workspace(q: torch.Tensor, k_new: torch.Tensor, max_nodes: int, max_len: int, batch: int) -> int:
+    """Bytes of workspace that op_tree_attn needs for these shapes."""
+    d = _tree_desc(q, k_new, 0, 0, 0, None)
+    n = load_library().first_op_tree_attn_workspace(C.byref(d), batch, q.shape[0], max_nodes, max_len)
+    return n if n >= 0 else _raise(n)
+
+
+def op_tree_attn(q: torch.Tensor, k_new: torch.Tensor, v_new: torch.Tensor, kv_layer: Optional[torch.Tensor], page_table: Optional[torch.Tensor],
+                 lens: torch.Tensor, node_offsets: torch.Tensor, out: torch.Tensor, max_nodes: int, max_len: int, mask: Optional[torch.Tensor] = None,
+                 scale: Optional[float] = None, lse: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None, stream=None) -> None:
+    """Attention of drafted tokens q [N, heads, head_dim] over one layer's pages kv_layer [pages, 2, KV heads, 16, head_dim] and over the tree's own
+    k_new, v_new [N, KV heads, head_dim].  page_table int32 [B, pages a sequence], lens int32 [B], node_offsets int32 [B + 1]; mask int64
+    [N, words], bit j of a node's row: it sees node j of its sequence (None: a chain).  scale None: 1 / sqrt(head_dim)."""
+    lib = load_library()
+    N, hq, hd = q.shape
+    B, hkv = lens.shape[0], k_new.shape[1]
+    pages, max_pages = (0, 0) if kv_layer is None or page_table is None else (kv_layer.shape[0], page_table.shape[1])
+    d = _tree_desc(q, k_new, pages, max_pages, 0 if mask is None else mask.shape[1], scale)
+    ptrs = [_same(q, q.dtype, (N, hq, hd), q, "q"), _same(k_new, q.dtype, (N, hkv, hd), q, "k_new"), _same(v_new, q.dtype, (N, hkv, hd), q, "v_new"),
+            0 if kv_layer is None else _same(kv_layer, q.dtype, (pages if pages else kv_layer.shape[0], 2, hkv, 16, hd), q, "kv_layer"),
+            0 if page_table is None else _same(page_table, torch.int32, (B, page_table.shape[1]), q, "page_table"),
+            _same(lens, torch.int32, (B,), q, "lens"), _same(node_offsets, torch.int32, (B + 1,), q, "node_offsets"),
+            0 if mask is None else _same(mask, torch.int64, (N, mask.shape[1]), q, "mask"), _same(out, q.dtype, (N, hq, hd), q, "out"),
+            0 if lse is None else _same(lse, torch.float32, (N, hq), q, "lse")]
+    on = _On(q, stream)
+    with on as st:
+        ws, size = on.workspace(workspace, lib.first_op_tree_attn_workspace(C.byref(d), B, N, max_nodes, max_len))
+        rc = lib.first_op_tree_attn(st, C.byref(d), *ptrs, B, N, max_nodes, max_len, ws, size)
+    if rc != 0:
+        _raise(rc)
+
+
+def sample_workspace(logits: torch.Tensor) -> int:
+    """Bytes of workspace that sample needs for these logits."""
+    n = load_library().first_sample_workspace(logits.shape[0], logits.shape[1])
+    return n if n >= 0 else _raise(n)
+
+
+def sample(logits: torch.Tensor, uniforms: torch.Tensor, token: torch.Tensor, temperature: Optional[torch.Tensor] = None,
+           top_k: Optional[torch.Tensor] = None, top_p: Optional[torch.Tensor] = None, min_p: Optional[torch.Tensor] = None,
+           logprob: Optional[torch.Tensor] = None, kept: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None, stream=None) -> None:
+    """A token a row of logits [rows, vocab] (fp32; the rows may be strided), by the row's own temperature, top_k, top_p, min_p (None: off) and
+    uniform number; token, kept int32, logprob fp32 [rows]."""
+    lib = load_library()
+    rows, vocab = logits.shape
+    if logits.dtype != torch.float32 or (logits.numel() > 0 and vocab > 1 and logits.stride(1) != 1):
+        raise ValueError("logits: expected float32, the logits of a row one after the other")
+    f, i = torch.float32, torch.int32
+    opt = lambda t, dtype, name: 0 if t is None else _same(t, dtype, (rows,), logits, name)  # noqa: E731
+    ptrs = [_same(uniforms, f, (rows,), logits, "uniforms"), opt(temperature, f, "temperature"), opt(top_k, i, "top_k"), opt(top_p, f, "top_p"),
+            opt(min_p, f, "min_p"), _same(token, i, (rows,), logits, "token"), opt(logprob, f, "logprob"), opt(kept, i, "kept")]
+    on = _On(logits, stream)
+    with on as st:
+        ws, size = on.workspace(workspace, lib.first_sample_workspace(rows, vocab))
+        rc = lib.first_sample(st, logits.data_ptr(), logits.stride(0) if rows > 1 else vocab, rows, vocab, *ptrs, ws, size)
+    if rc != 0:
+        _raise(rc)

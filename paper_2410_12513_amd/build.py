@@ -1,13 +1,17 @@
 """Builds libfirst.so (the C-ABI HIP library) for gfx950 with hipcc, in-tree."""
 from __future__ import annotations
 
+import concurrent.futures
 import os
 import re
 import subprocess
 import sys
+import tempfile
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 SRC = os.path.join(HERE, "csrc", "first_api.hip")
+OPS_SRC = os.path.join(HERE, "csrc", "ops_api.hip")      # the operators without a context
+SOURCES = (SRC, OPS_SRC)
 LIB = os.path.join(HERE, "libfirst.so")
 
 # -packed-fp32-ops is switched off for all device code of this library.
@@ -69,24 +73,34 @@ def over_limits(resources: dict) -> list:
 
 def build(verbose: bool = False) -> str:
     hipcc = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
-    cmd = [hipcc] + FLAGS + [SRC, "-o", LIB + ".tmp"]
-    res = subprocess.run(cmd, capture_output=True, text=True)
-    kept, skip = [], 0
-    for l in res.stderr.splitlines():                  # drop the resource remarks (each followed by a source line and a caret line)
-        if "kernel-resource-usage" in l:
-            skip = 2
-        elif skip and re.match(r"\s+(\d+ )?\|", l):
-            skip -= 1
-        elif "packed-fp32-ops" not in l and not l.startswith("In file included from"):
-            skip = 0
-            kept.append(l)
-    err = "\n".join(kept)
-    if res.returncode != 0:
-        raise RuntimeError("hipcc failed:\n" + err)
-    over = over_limits(kernel_resources(res.stderr))
-    if over:
-        os.remove(LIB + ".tmp")
-        raise RuntimeError("\n".join(over))
+    with tempfile.TemporaryDirectory() as tmp:
+        objects = [os.path.join(tmp, os.path.basename(src) + ".o") for src in SOURCES]
+        compile_flags = [f for f in FLAGS if f != "-shared"]
+        with concurrent.futures.ThreadPoolExecutor(len(SOURCES)) as pool:      # a compiler each
+            results = list(pool.map(lambda so: subprocess.run([hipcc] + compile_flags + ["-c", so[0], "-o", so[1]], capture_output=True, text=True),
+                                    zip(SOURCES, objects)))
+        err, remarks = [], ""
+        for res in results:
+            remarks += res.stderr
+            kept, skip = [], 0
+            for l in res.stderr.splitlines():          # drop the resource remarks (each followed by a source line and a caret line)
+                if "kernel-resource-usage" in l:
+                    skip = 2
+                elif skip and re.match(r"\s+(\d+ )?\|", l):
+                    skip -= 1
+                elif "packed-fp32-ops" not in l and not l.startswith("In file included from"):
+                    skip = 0
+                    kept.append(l)
+            err += kept
+        err = "\n".join(err)
+        if any(res.returncode != 0 for res in results):
+            raise RuntimeError("hipcc failed:\n" + err)
+        over = over_limits(kernel_resources(remarks))
+        if over:
+            raise RuntimeError("\n".join(over))
+        res = subprocess.run([hipcc, "--offload-arch=gfx950", "-fPIC", "-shared"] + objects + ["-o", LIB + ".tmp"], capture_output=True, text=True)
+        if res.returncode != 0:
+            raise RuntimeError("hipcc failed to link:\n" + res.stderr)
     if verbose and err.strip():
         sys.stderr.write(err + "\n")
     os.replace(LIB + ".tmp", LIB)

@@ -11,6 +11,7 @@
 #include <vector>
 
 #include "../../include/first.h"
+#include "last_error.h"
 #include "decode_kernels.h"
 #include "prefill_kernels.h"
 #include "step_kernel.h"
@@ -37,9 +38,9 @@ static __device__ __align__(256) unsigned char scratch[STATIC_SCRATCH_CANDS * 8]
 static void* g_scratch_ptr[STATIC_SCRATCH_MAX_DEV] = {};
 static std::mutex g_scratch_mutex;
 
-namespace {
+namespace first { thread_local std::string g_create_error; }
 
-thread_local std::string g_create_error;
+namespace {
 
 struct HipOrderApi {
   using Stream = hipStream_t;
