@@ -351,7 +351,7 @@ int first_op_gemm_nt_f32a(void *hip_stream, const float *A, const void *W, float
  * row is the shared projection alone.
  *   A DEV [m, k], W DEV [n, k], La DEV [n_adapters, r, k], Lb DEV [n_adapters, n, r] of dtype, on 16 bytes; adapter DEV int32 [m];
  *   scale DEV fp32 [n_adapters] (lora_alpha / r); C DEV fp32 [m, n], which none of the others may overlap; k multiple of 8; 1 <= r <= 64.
- *   m <= 2^20.  Adapters of smaller ranks: zeros in the rest of La or Lb.
+ *   m, n, k <= 2^20.  Adapters of smaller ranks: zeros in the rest of La or Lb.
  * Products of bf16 values are exact, all sums fp32; La A[i] stays in fp32 (bf16: three bf16 parts, which is all of it). */
 int64_t first_op_gemm_nt_lora_workspace(int32_t dtype, int32_t m, int32_t n, int32_t k, int32_t r);
 int first_op_gemm_nt_lora(void *hip_stream, int32_t dtype, const void *A, const void *W, const void *La, const void *Lb,
@@ -401,10 +401,10 @@ typedef struct first_tree_attn_desc {
  *   page_table   DEV int32 [B, max_pages]; a page outside [0, n_pages) holds nothing: its positions are not seen
  *   lens         DEV int32 [B], taken as at most max_len and 16 max_pages, and as 0 below it.  Cached positions >= lens[b] are never used, whatever
  *                they hold, nor is what stands in k_new / v_new at nodes that a node does not see, infinities and NaN included
- *   node_offsets DEV int32 [B + 1], ascending; of a sequence's nodes the first max_nodes are computed, rows of other nodes stay as they are
+ *   node_offsets DEV int32 [B + 1], ascending, max_nodes <= 2048; of a sequence's nodes the first max_nodes are computed, rows of other nodes stay as they are
  *   tree_mask    DEV uint64 [N, mask_words], mask_words * 64 >= max_nodes (may be NULL)
  *   lse          DEV fp32 [N, n_q_heads] (may be NULL)
- * N = node_offsets[B], max_nodes and max_len are bounds that the host knows; out must overlap nothing else. */
+ * max_len <= 2^28.  N = node_offsets[B], max_nodes and max_len are bounds that the host knows; out must overlap nothing else. */
 int64_t first_op_tree_attn_workspace(const first_tree_attn_desc *desc, int32_t B, int32_t N, int32_t max_nodes, int32_t max_len);
 int first_op_tree_attn(void *hip_stream, const first_tree_attn_desc *desc, const void *q, const void *k_new, const void *v_new,
                        const void *kv_layer, const int32_t *page_table, const int32_t *lens, const int32_t *node_offsets,

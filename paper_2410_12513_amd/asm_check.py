@@ -5,7 +5,7 @@ loads stay in flight across barriers and other work.  The compiler believes such
 value from the asm statement on.  If it touches the register before the wait that covers the load - because the value
 is dead, or spilled, or MOVED TO ANOTHER REGISTER (live-range splitting at a branch does that) - it reads or overwrites
 something that is not there yet; one such copy gave wrong attention results on the first decode step of a sequence, when
-memory is slow, and a reused register once ended in a memory fault.  This module compiles the library's source to
+memory is slow, and a reused register once ended in a memory fault.  This module compiles the library's sources to
 assembly and walks every kernel whose name contains one of the given keys.  Loads inside an inline asm statement (hipcc
 brackets those with ;;#ASMSTART / ;;#ASMEND) are "in flight" until a vmcnt wait covers them - every vector memory
 operation counts, in issue order: `vmcnt(N)` leaves the N youngest outstanding - and no instruction may name their
@@ -19,9 +19,10 @@ import re
 import subprocess
 import tempfile
 
-from .build import FLAGS, SRC
+from .build import FLAGS, SOURCES, SRC
 
-KERNELS = ("k_step", "k_attn_tiles_b", "k_attn_mfma_b", "k_batch_step", "k_bgemv", "k_gemm_nt_bf16_hl", "k_pgemm", "k_attn_prompt")
+KERNELS = ("k_step", "k_attn_tiles_b", "k_attn_mfma_b", "k_batch_step", "k_bgemv", "k_gemm_nt_bf16_hl", "k_pgemm", "k_attn_prompt",
+           "k_tree_attn", "k_lora_stream", "k_lora_tile")
 
 
 def _regs(tok: str):
@@ -33,15 +34,19 @@ def _regs(tok: str):
 
 
 def assembly() -> str:
+    """The device code of the library's sources, one after the other."""
     hipcc = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
     flags = [f for f in FLAGS if f not in ("-fPIC", "-shared", "-Rpass-analysis=kernel-resource-usage")]
+    text = []
     with tempfile.TemporaryDirectory() as tmp:
-        out = os.path.join(tmp, "first.s")
-        res = subprocess.run([hipcc] + flags + ["-S", "--cuda-device-only", SRC, "-o", out], capture_output=True, text=True, cwd=tmp)
-        if res.returncode != 0:
-            raise RuntimeError("hipcc -S failed:\n" + res.stderr[-2000:])
-        with open(out) as fh:
-            return fh.read()
+        for src in SOURCES:
+            out = os.path.join(tmp, os.path.basename(src) + ".s")
+            res = subprocess.run([hipcc] + flags + ["-S", "--cuda-device-only", src, "-o", out], capture_output=True, text=True, cwd=tmp)
+            if res.returncode != 0:
+                raise RuntimeError("hipcc -S failed:\n" + res.stderr[-2000:])
+            with open(out) as fh:
+                text.append(fh.read())
+    return "\n".join(text)
 
 
 def _functions(asm: str, keys):

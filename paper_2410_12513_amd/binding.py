@@ -3,6 +3,7 @@ device memory and the stream, nothing is computed here."""
 from __future__ import annotations
 
 import ctypes as C
+import functools
 import os
 from typing import List, Optional, Sequence
 
@@ -370,54 +371,58 @@ def sample_top_k_static(logits: torch.Tensor, uniforms: torch.Tensor, temperatur
 
 
 # ---- operators of a step over drafted tokens (stateless; stream=None: the current stream of the tensors' device) --------------
-
-
-class _On:
-    """The device of `t` current, and the stream to launch on: that of `stream`, or the device's current one."""
-
-    def __init__(self, t: torch.Tensor, stream):
-        if not t.is_cuda:
-            raise ValueError("expected device tensors")
-        self.guard = torch.cuda.device(t.device)
-        self.stream, self.device = stream, t.device
-
-    def __enter__(self):
-        self.guard.__enter__()
-        if self.stream is None:
-            self.stream = torch.cuda.current_stream(self.device)
-        return self.stream.cuda_stream
-
-    def __exit__(self, *exc):
-        return self.guard.__exit__(*exc)
-
-    def workspace(self, given: Optional[torch.Tensor], need: int):
-        """(address, bytes) of the caller's workspace, or of one that lives until the stream is through with it."""
-        if need < 0:
-            _raise(need)
-        if given is None:
-            if need == 0:
-                return 0, 0
-            given = torch.empty(need, dtype=torch.uint8, device=self.device)
-            given.record_stream(self.stream)
-        elif given.device != self.device or not given.is_contiguous():
-            raise ValueError("workspace: expected a contiguous tensor on the device of the others")
-        return given.data_ptr(), given.numel() * given.element_size()
+# A call of the small ones takes the GPU a few microseconds, so the checks here are the cheap forms of what they ask.
 
 
 def _raise(rc: int) -> None:
     raise FirstError(int(rc), load_library().first_last_error(None).decode())
 
 
-def _same(t: torch.Tensor, dtype: torch.dtype, shape, like: torch.Tensor, name: str) -> int:
-    if t.dtype != dtype or t.device != like.device or not t.is_contiguous() or t.shape != shape:
-        raise ValueError(f"{name}: expected a contiguous tensor of {dtype}, {list(shape)}, on {like.device}")
+def _device(t: torch.Tensor) -> int:
+    if not t.is_cuda:
+        raise ValueError("expected device tensors")
+    return t.get_device()
+
+
+def _same(t: torch.Tensor, dtype: torch.dtype, shape, dev: int, name: str) -> int:
+    """The address of a contiguous tensor of this type and shape on this device."""
+    if t.dtype is not dtype or t.shape != shape or not t.is_contiguous() or not t.is_cuda or t.get_device() != dev:
+        raise ValueError(f"{name}: expected a contiguous tensor of {dtype}, {list(shape)}, on device {dev}")
     return t.data_ptr()
 
 
 def _code(t: torch.Tensor, name: str) -> int:
-    if t.dtype not in (torch.bfloat16, torch.float32):
-        raise ValueError(f"{name}: expected bfloat16 or float32")
-    return DTYPE_CODES["bf16" if t.dtype == torch.bfloat16 else "fp32"]
+    if t.dtype is torch.bfloat16:
+        return 1
+    if t.dtype is torch.float32:
+        return 0
+    raise ValueError(f"{name}: expected bfloat16 or float32")
+
+
+def _launch(dev: int, stream, workspace: Optional[torch.Tensor], need, call) -> None:
+    """call(stream, workspace address, bytes) with device `dev` current, on `stream` or its current stream; a workspace of need() bytes lives until
+    that stream is through with it, unless the caller brings one."""
+    if torch.cuda.current_device() != dev:
+        with torch.cuda.device(dev):
+            return _launch(dev, stream, workspace, need, call)
+    st = torch.cuda.current_stream(dev).cuda_stream if stream is None else stream.cuda_stream
+    at = size = 0
+    if workspace is not None:
+        if workspace.get_device() != dev or not workspace.is_contiguous():
+            raise ValueError("workspace: expected a contiguous tensor on the device of the others")
+        at, size = workspace.data_ptr(), workspace.numel() * workspace.element_size()
+    elif need is not None:
+        size = need()
+        if size < 0:
+            _raise(size)
+        if size > 0:
+            workspace = torch.empty(size, dtype=torch.uint8, device=f"cuda:{dev}")
+            if stream is not None:
+                workspace.record_stream(stream)
+            at = workspace.data_ptr()
+    rc = call(st, at, size)
+    if rc != 0:
+        _raise(rc)
 
 
 def op_gemm_nt_lora_workspace(A: torch.Tensor, W: torch.Tensor, La: torch.Tensor) -> int:
@@ -430,19 +435,19 @@ def op_gemm_nt_lora(A: torch.Tensor, W: torch.Tensor, La: torch.Tensor, Lb: torc
                     accumulate: bool = False, workspace: Optional[torch.Tensor] = None, stream=None) -> None:
     """Cm[i] (+)= W A[i] + scale[a] Lb[a] (La[a] A[i]), a = adapter[i] (outside [0, adapters): none).  A [m, k], W [n, k], La [adapters, r, k],
     Lb [adapters, n, r] of one type; Cm fp32 [m, n]."""
-    lib = load_library()
-    code = _code(W, "W")
+    lib, code, dev, dtype = load_library(), _code(W, "W"), _device(W), W.dtype
     m, k = A.shape
-    n, (ads, r) = W.shape[0], La.shape[:2]
-    ptrs = [_same(A, W.dtype, (m, k), W, "A"), _same(W, W.dtype, (n, k), W, "W"), _same(La, W.dtype, (ads, r, k), W, "La"),
-            _same(Lb, W.dtype, (ads, n, r), W, "Lb"), _same(adapter, torch.int32, (m,), W, "adapter"), _same(scale, torch.float32, (ads,), W, "scale"),
-            _same(Cm, torch.float32, (m, n), W, "C")]
-    on = _On(W, stream)
-    with on as st:
-        ws, size = on.workspace(workspace, lib.first_op_gemm_nt_lora_workspace(code, m, n, k, r))
-        rc = lib.first_op_gemm_nt_lora(st, code, *ptrs, m, n, k, ads, r, int(accumulate), ws, size)
-    if rc != 0:
-        _raise(rc)
+    n, (ads, r, _) = W.shape[0], La.shape
+    ptrs = (_same(A, dtype, (m, k), dev, "A"), _same(W, dtype, (n, k), dev, "W"), _same(La, dtype, (ads, r, k), dev, "La"),
+            _same(Lb, dtype, (ads, n, r), dev, "Lb"), _same(adapter, torch.int32, (m,), dev, "adapter"), _same(scale, torch.float32, (ads,), dev, "scale"),
+            _same(Cm, torch.float32, (m, n), dev, "C"))
+    _launch(dev, stream, workspace, lambda: lib.first_op_gemm_nt_lora_workspace(code, m, n, k, r),
+            lambda st, ws, size: lib.first_op_gemm_nt_lora(st, code, *ptrs, m, n, k, ads, r, int(accumulate), ws, size))
+
+
+@functools.lru_cache(maxsize=256)
+def _rope_desc(*fields):
+    return _RopeDesc(*fields)
 
 
 def op_rope(x: torch.Tensor, positions: torch.Tensor, y: torch.Tensor, rot_dim: Optional[int] = None, layout: str = "half", base: float = 10000.0,
@@ -450,32 +455,30 @@ def op_rope(x: torch.Tensor, positions: torch.Tensor, y: torch.Tensor, rot_dim: 
             inverse: bool = False, stream=None) -> None:
     """Rotary positions of the heads of x [rows, heads, head_dim] into y (which may be x).  The rows may be strided: heads of a packed projection
     output.  inverse: turn back, which on a gradient is the backward pass."""
-    lib = load_library()
-    code = _code(x, "x")
+    lib, code, dev = load_library(), _code(x, "x"), _device(x)
     rows, heads, hd = x.shape
+    pitches = []
     for t, name in ((x, "x"), (y, "y")):
-        if t.dtype != x.dtype or t.device != x.device or t.shape != x.shape or (t.numel() > 0 and (t.stride(2) != 1 or (heads > 1 and t.stride(1) != hd))):
+        st = t.stride()
+        if t.dtype is not x.dtype or t.shape != x.shape or not t.is_cuda or t.get_device() != dev or (rows and (st[2] != 1 or (heads > 1 and st[1] != hd))):
             raise ValueError(f"{name}: expected [rows, heads, head_dim] of one type on one device, the heads of a row one after the other")
+        pitches.append(st[0] if rows > 1 else heads * hd)
     if layout not in ROPE_LAYOUTS or scaling not in ROPE_SCALINGS:
         raise ValueError(f"layout is one of {list(ROPE_LAYOUTS)}, scaling one of {list(ROPE_SCALINGS)}")
-    pos = _same(positions, torch.int32, (rows,), x, "positions")
-    d = _RopeDesc(code, heads, hd, hd if rot_dim is None else rot_dim, ROPE_LAYOUTS[layout], ROPE_SCALINGS[scaling], int(inverse), original_len, base, factor,
-                  low, high, amplitude)
-    pitch = lambda t: t.stride(0) if rows > 1 else heads * hd  # noqa: E731
-    with _On(x, stream) as st:
-        rc = lib.first_op_rope(st, C.byref(d), x.data_ptr(), pitch(x), y.data_ptr(), pitch(y), pos, rows)
-    if rc != 0:
-        _raise(rc)
+    pos = _same(positions, torch.int32, (rows,), dev, "positions")
+    d = _rope_desc(code, heads, hd, hd if rot_dim is None else rot_dim, ROPE_LAYOUTS[layout], ROPE_SCALINGS[scaling], int(inverse), original_len, base,
+                   factor, low, high, amplitude)
+    _launch(dev, stream, None, None, lambda st, ws, size: lib.first_op_rope(st, C.byref(d), x.data_ptr(), pitches[0], y.data_ptr(), pitches[1], pos, rows))
 
 
-def _tree_desc(q: torch.Tensor, k_new: torch.Tensor, pages: int, max_pages: int, words: int, scale: Optional[float]) -> _TreeAttnDesc:
-    hd = q.shape[2]
-    return _TreeAttnDesc(_code(q, "q"), q.shape[1], k_new.shape[1], hd, 16, pages, max_pages, words, hd ** -0.5 if scale is None else scale)
+@functools.lru_cache(maxsize=256)
+def _tree_desc(*fields):
+    return _TreeAttnDesc(*fields)
 
 
 def op_tree_attn_workspace(q: torch.Tensor, k_new: torch.Tensor, max_nodes: int, max_len: int, batch: int) -> int:
     """Bytes of workspace that op_tree_attn needs for these shapes."""
-    d = _tree_desc(q, k_new, 0, 0, 0, None)
+    d = _tree_desc(_code(q, "q"), q.shape[1], k_new.shape[1], q.shape[2], 16, 0, 0, 0, 1.0)
     n = load_library().first_op_tree_attn_workspace(C.byref(d), batch, q.shape[0], max_nodes, max_len)
     return n if n >= 0 else _raise(n)
 
@@ -486,23 +489,22 @@ def op_tree_attn(q: torch.Tensor, k_new: torch.Tensor, v_new: torch.Tensor, kv_l
     """Attention of drafted tokens q [N, heads, head_dim] over one layer's pages kv_layer [pages, 2, KV heads, 16, head_dim] and over the tree's own
     k_new, v_new [N, KV heads, head_dim].  page_table int32 [B, pages a sequence], lens int32 [B], node_offsets int32 [B + 1]; mask int64
     [N, words], bit j of a node's row: it sees node j of its sequence (None: a chain).  scale None: 1 / sqrt(head_dim)."""
-    lib = load_library()
+    lib, code, dev, dtype, i32 = load_library(), _code(q, "q"), _device(q), q.dtype, torch.int32
     N, hq, hd = q.shape
     B, hkv = lens.shape[0], k_new.shape[1]
-    pages, max_pages = (0, 0) if kv_layer is None or page_table is None else (kv_layer.shape[0], page_table.shape[1])
-    d = _tree_desc(q, k_new, pages, max_pages, 0 if mask is None else mask.shape[1], scale)
-    ptrs = [_same(q, q.dtype, (N, hq, hd), q, "q"), _same(k_new, q.dtype, (N, hkv, hd), q, "k_new"), _same(v_new, q.dtype, (N, hkv, hd), q, "v_new"),
-            0 if kv_layer is None else _same(kv_layer, q.dtype, (pages if pages else kv_layer.shape[0], 2, hkv, 16, hd), q, "kv_layer"),
-            0 if page_table is None else _same(page_table, torch.int32, (B, page_table.shape[1]), q, "page_table"),
-            _same(lens, torch.int32, (B,), q, "lens"), _same(node_offsets, torch.int32, (B + 1,), q, "node_offsets"),
-            0 if mask is None else _same(mask, torch.int64, (N, mask.shape[1]), q, "mask"), _same(out, q.dtype, (N, hq, hd), q, "out"),
-            0 if lse is None else _same(lse, torch.float32, (N, hq), q, "lse")]
-    on = _On(q, stream)
-    with on as st:
-        ws, size = on.workspace(workspace, lib.first_op_tree_attn_workspace(C.byref(d), B, N, max_nodes, max_len))
-        rc = lib.first_op_tree_attn(st, C.byref(d), *ptrs, B, N, max_nodes, max_len, ws, size)
-    if rc != 0:
-        _raise(rc)
+    if (kv_layer is None) != (page_table is None):
+        raise ValueError("kv_layer and page_table come together")
+    pages, width = (0, 0) if kv_layer is None else (kv_layer.shape[0], page_table.shape[1])
+    words = 0 if mask is None else mask.shape[1]
+    d = _tree_desc(code, hq, hkv, hd, 16, pages, width, words, hd ** -0.5 if scale is None else scale)
+    ptrs = (_same(q, dtype, (N, hq, hd), dev, "q"), _same(k_new, dtype, (N, hkv, hd), dev, "k_new"), _same(v_new, dtype, (N, hkv, hd), dev, "v_new"),
+            0 if kv_layer is None else _same(kv_layer, dtype, (pages, 2, hkv, 16, hd), dev, "kv_layer"),
+            0 if page_table is None else _same(page_table, i32, (B, width), dev, "page_table"),
+            _same(lens, i32, (B,), dev, "lens"), _same(node_offsets, i32, (B + 1,), dev, "node_offsets"),
+            0 if mask is None else _same(mask, torch.int64, (N, words), dev, "mask"), _same(out, dtype, (N, hq, hd), dev, "out"),
+            0 if lse is None else _same(lse, torch.float32, (N, hq), dev, "lse"))
+    _launch(dev, stream, workspace, lambda: lib.first_op_tree_attn_workspace(C.byref(d), B, N, max_nodes, max_len),
+            lambda st, ws, size: lib.first_op_tree_attn(st, C.byref(d), *ptrs, B, N, max_nodes, max_len, ws, size))
 
 
 def sample_workspace(logits: torch.Tensor) -> int:
@@ -516,17 +518,14 @@ def sample(logits: torch.Tensor, uniforms: torch.Tensor, token: torch.Tensor, te
            logprob: Optional[torch.Tensor] = None, kept: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None, stream=None) -> None:
     """A token a row of logits [rows, vocab] (fp32; the rows may be strided), by the row's own temperature, top_k, top_p, min_p (None: off) and
     uniform number; token, kept int32, logprob fp32 [rows]."""
-    lib = load_library()
+    lib, f, i = load_library(), torch.float32, torch.int32
     rows, vocab = logits.shape
-    if logits.dtype != torch.float32 or (logits.numel() > 0 and vocab > 1 and logits.stride(1) != 1):
+    if logits.dtype is not f or (rows and vocab > 1 and logits.stride(1) != 1):
         raise ValueError("logits: expected float32, the logits of a row one after the other")
-    f, i = torch.float32, torch.int32
-    opt = lambda t, dtype, name: 0 if t is None else _same(t, dtype, (rows,), logits, name)  # noqa: E731
-    ptrs = [_same(uniforms, f, (rows,), logits, "uniforms"), opt(temperature, f, "temperature"), opt(top_k, i, "top_k"), opt(top_p, f, "top_p"),
-            opt(min_p, f, "min_p"), _same(token, i, (rows,), logits, "token"), opt(logprob, f, "logprob"), opt(kept, i, "kept")]
-    on = _On(logits, stream)
-    with on as st:
-        ws, size = on.workspace(workspace, lib.first_sample_workspace(rows, vocab))
-        rc = lib.first_sample(st, logits.data_ptr(), logits.stride(0) if rows > 1 else vocab, rows, vocab, *ptrs, ws, size)
-    if rc != 0:
-        _raise(rc)
+    dev, shape = _device(logits), (rows,)
+    ptrs = (_same(uniforms, f, shape, dev, "uniforms"), 0 if temperature is None else _same(temperature, f, shape, dev, "temperature"),
+            0 if top_k is None else _same(top_k, i, shape, dev, "top_k"), 0 if top_p is None else _same(top_p, f, shape, dev, "top_p"),
+            0 if min_p is None else _same(min_p, f, shape, dev, "min_p"), _same(token, i, shape, dev, "token"),
+            0 if logprob is None else _same(logprob, f, shape, dev, "logprob"), 0 if kept is None else _same(kept, i, shape, dev, "kept"))
+    _launch(dev, stream, workspace, lambda: lib.first_sample_workspace(rows, vocab),
+            lambda st, ws, size: lib.first_sample(st, logits.data_ptr(), logits.stride(0) if rows > 1 else vocab, rows, vocab, *ptrs, ws, size))

@@ -2,6 +2,7 @@
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
+#include <atomic>
 #include <cmath>
 
 #include "../../include/first.h"
@@ -20,8 +21,9 @@ int refuse(int code, const char* text) noexcept {
   try { g_create_error = text; } catch (...) {}
   return code;
 }
-int launched(const char* name) noexcept {
-  const hipError_t e = hipGetLastError();
+int launched(const char* name, hipError_t e = hipSuccess) noexcept {
+  const hipError_t last = hipGetLastError();
+  if (e == hipSuccess) e = last;
   if (e == hipSuccess) return FIRST_OK;
   try { g_create_error = std::string(name) + ": " + hipGetErrorString(e); } catch (...) {}
   return FIRST_ERR_HIP;
@@ -31,6 +33,104 @@ bool aligned(const void* p, size_t to) { return reinterpret_cast<uintptr_t>(p) %
 hipStream_t stream_of(void* s) { return reinterpret_cast<hipStream_t>(s); }
 size_t size_of(int dtype) { return dtype == FIRST_DTYPE_BF16 ? 2 : 4; }
 int64_t up(int64_t x, int64_t to) { return (x + to - 1) / to * to; }
+
+constexpr int CUS = 256;                  // compute units of the MI355X
+
+// Launches; a kernel that may use more than 64 KB of LDS is told so first, once a device.
+template <auto kernel, typename Args> hipError_t launch(hipStream_t st, dim3 grid, int threads, size_t lds, const Args& P) {
+  if (lds > 64 * 1024) {
+    static std::atomic<uint64_t> told{0};
+    int dev = 0;
+    hipError_t e = hipGetDevice(&dev);
+    if (e != hipSuccess) return e;
+    if (dev >= 64 || !(told.load(std::memory_order_relaxed) >> dev & 1)) {
+      e = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
+      if (e != hipSuccess) return e;
+      if (dev < 64) told.fetch_or(1ull << dev, std::memory_order_relaxed);
+    }
+  }
+  hipLaunchKernelGGL(kernel, grid, dim3(threads), lds, st, P);
+  return hipGetLastError();
+}
+
+// ---- projections with an adapter per row -----------------------------------------------------------------------------------
+// stream: up to 32 rows, slices of K such that two workgroups a compute unit are busy, of four steps at least.  tile: the BM x BN with the least estimated time, rounds
+// of the chip times the tile's products over how well it feeds the matrix cores; slices of K where the tiles of one round leave half of the chip idle.
+struct LoraPlan { int tile, ks; };        // tile 0: stream
+LoraPlan lora_plan(int dtype, int m, int n, int k) {
+  const int64_t steps = up((int64_t)k * size_of(dtype), 128) / 128;
+  if (m <= LORA_STREAM_ROWS) {
+    const int64_t groups = (n + 63) / 64;
+    return {0, (int)std::max<int64_t>(1, std::min<int64_t>({(2 * CUS + groups / 2) / groups, steps / 4, 16}))};
+  }
+  LoraPlan best = {64, 1};
+  double least = 1e300;
+  for (int t : {256, 128, 64}) {
+    const int64_t tiles = (int64_t)((m + t - 1) / t) * ((n + t - 1) / t);
+    const int64_t ks = m > 65535 ? 1 : std::max<int64_t>(1, std::min<int64_t>({CUS / tiles, steps / 8, 8}));
+    const double feed = t == 256 ? 1.0 : t == 128 ? 0.75 : 0.45, rounds = (double)((tiles * ks + CUS - 1) / CUS);
+    const double time = rounds * ((double)t * t / feed * ((steps + ks - 1) / ks) + 8 * t * t) + (ks > 1 ? 2e5 : 0);
+    if (time < least) { least = time; best = {t, (int)ks}; }
+  }
+  return best;
+}
+int64_t lora_t_bytes(int m, int r) { return up((int64_t)m * up(r, 16) * 4, 256); }
+template <typename E> hipError_t launch_lora(hipStream_t st, LoraArgs& P, const LoraPlan& plan) {
+  P.shrink_tiles = (P.m + 15) / 16;
+  P.shrink_ways = std::max(1, std::min(16, CUS / P.shrink_tiles));
+  const int helpers = P.shrink_tiles * P.shrink_ways;
+  P.ks = plan.ks;
+  hipError_t e;
+  if (plan.tile == 0) {
+    const int grid = helpers + (P.n + 63) / 64 * P.ks;
+    e = P.m <= 16 ? launch<&k_lora_stream<E, 16, 4>>(st, grid, WG, 4 * 4 * 32 * 128, P) : launch<&k_lora_stream<E, 32, 3>>(st, grid, WG, 4 * 3 * 48 * 128, P);
+  } else {
+    e = launch<&k_lora_shrink<E>>(st, helpers, LORA_SHRINK_WAVES * 64, (size_t)LORA_SHRINK_WAVES * 16 * P.rp * 4, P);
+    if (e != hipSuccess) return e;
+    P.gm = (P.m + plan.tile - 1) / plan.tile;
+    P.gn = (P.n + plan.tile - 1) / plan.tile;
+    const int grid = P.gm * P.gn * P.ks;
+    e = plan.tile == 256 ? launch<&k_lora_tile<E, 256, 256, 4, 2, 64, 4>>(st, grid, 512, 4 * 512 * 64, P)
+        : plan.tile == 128 ? launch<&k_lora_tile<E, 128, 128, 2, 2, 128, 4>>(st, grid, 256, 4 * 256 * 128, P)
+                           : launch<&k_lora_tile<E, 64, 64, 2, 2, 128, 4>>(st, grid, 256, 4 * 128 * 128, P);
+  }
+  if (e == hipSuccess && (plan.tile == 0 || P.ks > 1)) e = launch<&k_lora_finish<E>>(st, dim3((P.n + WG - 1) / WG, P.m), WG, 0, P);
+  return e;
+}
+
+// ---- attention of drafted tokens -------------------------------------------------------------------------------------------
+// Rows of a workgroup: the smallest block that holds a sequence's nodes times the query heads of a KV head, up to 256, as its keys are then
+// read once.  Splits: as many as fill the chip's places for workgroups once (by LDS: two a compute unit up to 80 KB, else one), of whole 128 keys.
+struct TreePlan { int block, split_keys, splits, row_blocks; };
+TreePlan tree_plan(const first_tree_attn_desc& d, int B, int max_nodes, int max_len) {
+  const int64_t rows = (int64_t)max_nodes * (d.n_q_heads / d.n_kv_heads);
+  const bool wide = d.dtype == FIRST_DTYPE_BF16;
+  TreePlan p;
+  p.block = rows <= 32 ? 32 : wide && rows <= 64 ? 64 : !wide || rows <= 128 ? 128 : 256;
+  p.row_blocks = (int)((rows + p.block - 1) / p.block);
+  const int places = CUS * (wide && (p.block == 64 || p.block == 128 || d.head_dim == 64) ? 2 : 1);
+  const int64_t base = std::max<int64_t>(1, (int64_t)B * d.n_kv_heads * p.row_blocks);
+  const int64_t want = std::max<int64_t>(1, places / base);
+  p.split_keys = (int)std::min<int64_t>(TREE_SPLIT_MAX, std::max<int64_t>(128, up((max_len + want - 1) / want, 128)));
+  p.splits = std::max(1, (max_len + p.split_keys - 1) / p.split_keys);
+  return p;
+}
+template <typename E, int HD, int QG, int KH, int NS, int S> hipError_t launch_tree_walk(hipStream_t st, const TreeArgs& P, const TreePlan& p) {
+  return launch<&k_tree_attn<E, HD, QG, KH, NS, S>>(st, dim3(P.Hkv * p.row_blocks, p.splits, P.B), QG * KH * 64, (size_t)S * 2 * KH * NS * 32 * HD * sizeof(E), P);
+}
+template <typename E, int HD> hipError_t launch_tree(hipStream_t st, const TreeArgs& P, const TreePlan& p) {
+  hipError_t e;
+  if constexpr (sizeof(E) == 2) {
+    e = p.block == 32 ? launch_tree_walk<E, HD, 1, 4, 1, 2>(st, P, p) : p.block == 64 ? launch_tree_walk<E, HD, 2, 2, 1, 2>(st, P, p)
+        : p.block == 128 ? launch_tree_walk<E, HD, 4, 1, 2, 2>(st, P, p) : launch_tree_walk<E, HD, 8, 1, 2, 3>(st, P, p);
+  } else {
+    e = p.block == 32 ? launch_tree_walk<E, HD, 1, 2, 1, 2>(st, P, p) : launch_tree_walk<E, HD, 4, 1, 2, 2>(st, P, p);
+  }
+  if (e == hipSuccess && p.splits > 1) {
+    e = launch<&k_tree_join<E, HD>>(st, dim3((P.max_nodes * P.Hq + WAVES - 1) / WAVES, P.B), WG, 0, P);
+  }
+  return e;
+}
 
 }  // namespace
 
@@ -88,7 +188,8 @@ int first_op_rope(void* hip_stream, const first_rope_desc* d, const void* x, int
 int64_t first_op_gemm_nt_lora_workspace(int32_t dtype, int32_t m, int32_t n, int32_t k, int32_t r) {
   if (!known_type(dtype) || m < 0 || n < 1 || k < 8 || k % 8 || r < 1 || r > LORA_RMAX)
     return refuse(FIRST_ERR_ARG, "first_op_gemm_nt_lora_workspace: unknown dtype, negative m, n < 1, k not a positive multiple of 8, or rank outside 1..64");
-  return up((int64_t)m * up(r, 16) * 4, 256);
+  const LoraPlan plan = lora_plan(dtype, m, n, k);
+  return m == 0 ? 0 : lora_t_bytes(m, r) + (plan.tile == 0 || plan.ks > 1 ? (int64_t)plan.ks * m * n * 4 : 0);
 }
 
 int first_op_gemm_nt_lora(void* hip_stream, int32_t dtype, const void* A, const void* W, const void* La, const void* Lb, const int32_t* adapter,
@@ -102,18 +203,11 @@ int first_op_gemm_nt_lora(void* hip_stream, int32_t dtype, const void* A, const 
   if (!aligned(A, 16) || !aligned(W, 16) || !aligned(La, 16) || !aligned(Lb, 16) || !aligned(workspace, 16) || !aligned(C, 4) || !aligned(adapter, 4) || !aligned(scale, 4))
     return refuse(FIRST_ERR_ARG, "first_op_gemm_nt_lora: A, W, La, Lb and the workspace must be on 16 bytes, the others on 4");
   if (workspace_bytes < need) return refuse(FIRST_ERR_CAPACITY, "first_op_gemm_nt_lora: the workspace is smaller than first_op_gemm_nt_lora_workspace says");
-  if (m > 1 << 20) return refuse(FIRST_ERR_CAPACITY, "first_op_gemm_nt_lora: too many rows");
-  LoraArgs P = {A, W, La, Lb, adapter, scale, C, (float*)workspace, m, n, k, r, (int)up(r, 16), n_adapters, accumulate != 0};
-  const dim3 grid((n + 63) / 64, (m + 63) / 64);
-  hipStream_t st = stream_of(hip_stream);
-  if (dtype == FIRST_DTYPE_BF16) {
-    hipLaunchKernelGGL(k_lora_shrink<bf16>, dim3(m), dim3(WG), 0, st, P);
-    hipLaunchKernelGGL(k_lora_gemm<bf16>, grid, dim3(WG), 0, st, P);
-  } else {
-    hipLaunchKernelGGL(k_lora_shrink<float>, dim3(m), dim3(WG), 0, st, P);
-    hipLaunchKernelGGL(k_lora_gemm<float>, grid, dim3(WG), 0, st, P);
-  }
-  return launched("first_op_gemm_nt_lora");
+  if (m > 1 << 20 || n > 1 << 20 || k > 1 << 20) return refuse(FIRST_ERR_CAPACITY, "first_op_gemm_nt_lora: more than 2^20 rows or columns");
+  LoraArgs P = {A, W, La, Lb, adapter, scale, C, (float*)workspace, (float*)((char*)workspace + lora_t_bytes(m, r)), m, n, k, r, (int)up(r, 16), n_adapters, accumulate != 0};
+  const LoraPlan plan = lora_plan(dtype, m, n, k);
+  const hipStream_t st = stream_of(hip_stream);
+  return launched("first_op_gemm_nt_lora", dtype == FIRST_DTYPE_BF16 ? launch_lora<bf16>(st, P, plan) : launch_lora<float>(st, P, plan));
 }
 
 static int tree_refusal(const first_tree_attn_desc* d, int32_t B, int32_t N, int32_t max_nodes, int32_t max_len) {
@@ -125,12 +219,15 @@ static int tree_refusal(const first_tree_attn_desc* d, int32_t B, int32_t N, int
     return refuse(FIRST_ERR_ARG, "first_op_tree_attn: scale not finite, or a negative size");
   if (B < 0 || N < 0 || max_nodes < 0 || max_len < 0) return refuse(FIRST_ERR_ARG, "first_op_tree_attn: a negative size");
   if (B > 65535) return refuse(FIRST_ERR_CAPACITY, "first_op_tree_attn: more than 65535 sequences");
+  if (max_nodes > TREE_MAX_NODES || max_len > 1 << 28) return refuse(FIRST_ERR_CAPACITY, "first_op_tree_attn: more than 2048 nodes of a sequence, or 2^28 positions");
   return FIRST_OK;
 }
 
 int64_t first_op_tree_attn_workspace(const first_tree_attn_desc* d, int32_t B, int32_t N, int32_t max_nodes, int32_t max_len) {
   const int rc = tree_refusal(d, B, N, max_nodes, max_len);
-  return rc != FIRST_OK ? rc : 0;
+  if (rc != FIRST_OK) return rc;
+  const TreePlan p = tree_plan(*d, B, max_nodes, max_len);
+  return p.splits == 1 ? 0 : (int64_t)p.splits * N * d->n_q_heads * (d->head_dim + 2) * 4;
 }
 
 int first_op_tree_attn(void* hip_stream, const first_tree_attn_desc* d, const void* q, const void* k_new, const void* v_new, const void* kv_layer,
@@ -147,18 +244,18 @@ int first_op_tree_attn(void* hip_stream, const first_tree_attn_desc* d, const vo
     return refuse(FIRST_ERR_ARG, "first_op_tree_attn: a pointer is not aligned (16 bytes for q, k, v, out, the cache and the workspace)");
   if (tree_mask && (int64_t)d->mask_words * 64 < max_nodes) return refuse(FIRST_ERR_ARG, "first_op_tree_attn: mask_words * 64 is below max_nodes");
   if (workspace_bytes < need) return refuse(FIRST_ERR_CAPACITY, "first_op_tree_attn: the workspace is smaller than first_op_tree_attn_workspace says");
+  const TreePlan p = tree_plan(*d, B, max_nodes, max_len);
   TreeArgs P = {q, k_new, v_new, kv_layer, page_table, lens, node_offsets, (const unsigned long long*)tree_mask, out, lse, B, N, d->n_q_heads, d->n_kv_heads, d->n_pages,
-                cached ? d->max_pages : 0, d->mask_words, max_nodes, max_len, d->scale};
-  const dim3 grid(max_nodes, d->n_q_heads, B);
-  hipStream_t st = stream_of(hip_stream);
-  if (d->dtype == FIRST_DTYPE_BF16) {
-    if (d->head_dim == 128) hipLaunchKernelGGL((k_tree_rows<bf16, 128>), grid, dim3(WG), 0, st, P);
-    else hipLaunchKernelGGL((k_tree_rows<bf16, 64>), grid, dim3(WG), 0, st, P);
-  } else {
-    if (d->head_dim == 128) hipLaunchKernelGGL((k_tree_rows<float, 128>), grid, dim3(WG), 0, st, P);
-    else hipLaunchKernelGGL((k_tree_rows<float, 64>), grid, dim3(WG), 0, st, P);
+                cached ? d->max_pages : 0, d->mask_words, max_nodes, max_len, d->scale, p.split_keys, p.splits, nullptr, nullptr};
+  if (need > 0) {
+    P.part = (float*)workspace;
+    P.ml = P.part + (size_t)p.splits * N * d->n_q_heads * d->head_dim;
   }
-  return launched("first_op_tree_attn");
+  const hipStream_t st = stream_of(hip_stream);
+  hipError_t e;
+  if (d->dtype == FIRST_DTYPE_BF16) e = d->head_dim == 128 ? launch_tree<bf16, 128>(st, P, p) : launch_tree<bf16, 64>(st, P, p);
+  else e = d->head_dim == 128 ? launch_tree<float, 128>(st, P, p) : launch_tree<float, 64>(st, P, p);
+  return launched("first_op_tree_attn", e);
 }
 
 int64_t first_sample_workspace(int32_t rows, int32_t vocab) {

@@ -47,7 +47,27 @@ struct SrRow {                            // what a row's weights are made of
   __device__ __forceinline__ double log2w(float l) const { return l == lmax ? 0.0 : ((double)l - (double)lmax) * c; }
   // tokens that count at all: the weight is not 0 in 64 bits
   __device__ __forceinline__ bool counts(float l, double x) const { return l > -INFINITY && x > -1074.5; }
-  __device__ __forceinline__ unsigned long long mass(double x) const { return (unsigned long long)rint(ldexp(exp2(x), S)); }
+  // 2^x 2^e: the power series of 2^f, f the rest of x to the nearest whole number, to f^11 (6e-15 at f = 1/2)
+  __device__ __forceinline__ double power(double x, int e) const {
+    const double n = rint(x), f = x - n;
+    double p = 4.4455382718708115e-10;
+    p = fma(p, f, 7.0549116208011233e-9);
+    p = fma(p, f, 1.0178086009239700e-7);
+    p = fma(p, f, 1.3215486790144310e-6);
+    p = fma(p, f, 1.5252733804059840e-5);
+    p = fma(p, f, 1.5403530393381610e-4);
+    p = fma(p, f, 1.3333558146428443e-3);
+    p = fma(p, f, 9.6181291076284772e-3);
+    p = fma(p, f, 5.5504108664821580e-2);
+    p = fma(p, f, 2.4022650695910071e-1);
+    p = fma(p, f, 6.9314718055994531e-1);
+    p = fma(p, f, 1.0);
+    return ldexp(p, (int)n + e);
+  }
+  // (a sum with 2^52 has the whole number, rounded, in its low bits)
+  __device__ __forceinline__ unsigned long long mass(double x) const {
+    return (unsigned long long)__double_as_longlong(power(fmax(x, -200.0), S) + 4503599627370496.0) & 0xfffffffffffffull;
+  }
 };
 
 struct SrFound { float value; int index; SrSum through; };   // the token at which the sum passes the target, and the sum up to and with it
@@ -123,18 +143,329 @@ __device__ inline SrFound sr_find(const float* row, int V, int index_bits, const
   return {value, (int)at, before + SrSum{R.mass(R.log2w(value)), 1u}};
 }
 
+// ---- a row in three looks --------------------------------------------------------------------------------------------------
+// What can be drawn and where the cuts lie is decided among a few tokens, a list in LDS that is put in order; what is not on it only matters by its sum.
+//   with top_k (up to SR_TOPK), or few tokens: the k-th largest of the threads' (of groups' of 16 threads) own maxima is a bound that at least k tokens reach; the
+//     list is what reaches it, and no other weight is formed;
+//   else: a histogram of the masses over 2048 equal parts of the range of logits that weigh anything says in which part each cut lies, and in which few the draw
+//     can lie; the list is those parts' tokens.
+// A list that does not fit (masses of equal logits, logits that crowd one part) is left for the digit by digit search over the whole row.
+constexpr int SR_LIST = 4096, SR_TOPK = 960, SR_U = 4;
+struct __align__(4) SrFour { float v[4]; };               // (a row starts on 4 bytes)
+
+struct SrFast {
+  unsigned long long list[SR_LIST];
+  unsigned long long hist[SR_BINS];
+  unsigned long long wave[SR_WAVES], base_c, base_d, total, kept_mass;
+  int found, first_c, cut_p, cut_m, kept, pick, c1, c2, d1, d2;
+  unsigned count[SR_WAVES];
+  float lo[SR_WAVES], hi[SR_WAVES];
+};
+union SrLds { SrShared slow; SrFast fast; };
+
+// f(logit, index) of every logit of the row, a thread's four at a time, SR_U pieces in flight.
+template <typename F> __device__ __forceinline__ void sr_each(const float* row, int V, F f) {
+  const int pieces = V / 4, tid = threadIdx.x;
+  int i = tid;
+  for (; i + (SR_U - 1) * SR_THREADS < pieces; i += SR_U * SR_THREADS) {
+    SrFour x[SR_U];
+#pragma unroll
+    for (int u = 0; u < SR_U; ++u) x[u] = *reinterpret_cast<const SrFour*>(row + 4 * (i + u * SR_THREADS));
+#pragma unroll
+    for (int u = 0; u < SR_U; ++u)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) f(x[u].v[e], 4 * (i + u * SR_THREADS) + e);
+  }
+  for (; i < pieces; i += SR_THREADS) {
+    const SrFour x = *reinterpret_cast<const SrFour*>(row + 4 * i);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) f(x.v[e], 4 * i + e);
+  }
+  if (tid < V - 4 * pieces) f(row[4 * pieces + tid], 4 * pieces + tid);
+}
+__device__ __forceinline__ unsigned long long sr_key(float l, int i) { return (unsigned long long)sr_order(l) << 32 | (uint32_t)~i; }
+
+// list[0 .. n) into descending order, n <= SR_LIST.  Ends with a barrier.
+__device__ inline void sr_sort(unsigned long long* list, int n) {
+  const int tid = threadIdx.x;
+  if (n <= 512) {                                          // by rank: a key's place is the number of larger ones (all differ but for zeros)
+    const unsigned long long x = tid < n ? list[tid] : 0ull;
+    int before = 0;
+    if (tid < n)
+      for (int j = 0; j < n; ++j) before += list[j] > x;
+    __syncthreads();
+    if (tid < n) list[tid] = 0ull;                         // (places behind equal zeros)
+    __syncthreads();
+    if (tid < n) list[before] = x;
+    __syncthreads();
+    return;
+  }
+  int size = 1024;
+  while (size < n) size *= 2;
+  for (int i = n + tid; i < size; i += SR_THREADS) list[i] = 0ull;
+  __syncthreads();
+  for (int k = 2; k <= size; k *= 2)
+    for (int j = k / 2; j > 0; j /= 2) {
+      for (int t = tid; t < size / 2; t += SR_THREADS) {
+        const int i = 2 * j * (t / j) + t % j, o = i + j;
+        const unsigned long long a = list[i], b = list[o];
+        if ((a < b) == ((i & k) == 0)) { list[i] = b; list[o] = a; }
+      }
+      __syncthreads();
+    }
+}
+// Exclusive running sum over the threads, and the sum of all.
+__device__ __forceinline__ unsigned long long sr_scan(unsigned long long v, unsigned long long* wave, unsigned long long& all) {
+  const int tid = threadIdx.x;
+  unsigned long long incl = v;
+#pragma unroll
+  for (int d = 1; d < 64; d <<= 1) {
+    const unsigned long long o = (unsigned long long)__shfl_up((long long)incl, d, 64);
+    if ((tid & 63) >= d) incl += o;
+  }
+  __syncthreads();
+  if ((tid & 63) == 63) wave[tid >> 6] = incl;
+  __syncthreads();
+  unsigned long long base = 0;
+  all = 0;
+  for (int w = 0; w < SR_WAVES; ++w) {
+    if (w < tid >> 6) base += wave[w];
+    all += wave[w];
+  }
+  return base + incl - v;
+}
+// Whole numbers of a fraction of a mass: what a running sum has to reach (at least 1), and what it has to pass.
+__device__ __forceinline__ unsigned long long sr_reach(float p, unsigned long long total) {
+  const double want = ceil(fmax((double)p, 0.0) * (double)total);
+  const unsigned long long x = want < 1.0 ? 1ull : (unsigned long long)want;
+  return x < total ? x : total;
+}
+__device__ __forceinline__ unsigned long long sr_pass(float u, unsigned long long total) {
+  const double want = floor(fmax((double)u, 0.0) * (double)total);
+  const unsigned long long x = want < (double)total ? (unsigned long long)want : total;
+  return x < total ? x : total - 1;
+}
+
+struct SrRules { float u, top_p, min_p; int top_k; bool greedy; };
+struct SrOut { int token; float value; unsigned long long kept_mass; int kept; };
+
+struct SrFirst { float value; int index; };                // a thread's own largest logit
+// False: the list did not fit.
+__device__ inline bool sr_fast(const float* row, int V, const SrRow& R, const SrRules& Q, SrFirst first, float lmin, SrFast& sh, SrOut& out) {
+  const int tid = threadIdx.x;
+  const bool by_prefix = Q.top_k > 0 && Q.top_k <= SR_TOPK, whole = V <= SR_LIST;
+  const bool cut_p = !Q.greedy && Q.top_p < 1.f, cut_m = !Q.greedy && Q.min_p > 0.f;
+  if (Q.top_k > SR_TOPK && Q.top_k < V && !whole) return false;
+  if (tid == 0) { sh.found = 0; sh.first_c = 0; sh.base_c = sh.base_d = 0ull; sh.c1 = 0; sh.c2 = SR_BINS; sh.d1 = 0; sh.d2 = SR_BINS; }
+  __syncthreads();
+  if (whole || by_prefix) {
+    unsigned long long bound = 0ull;
+    if (!whole) {
+      unsigned long long own = first.value > -INFINITY ? sr_key(first.value, first.index) : 0ull;
+      if (Q.top_k <= 64) {                                 // groups of 16 threads
+#pragma unroll
+        for (int d = 8; d > 0; d >>= 1) {
+          const unsigned long long o = (unsigned long long)__shfl_xor((long long)own, d, 64);
+          own = o > own ? o : own;
+        }
+        if ((tid & 15) == 0) sh.list[tid >> 4] = own;
+      } else {
+        sh.list[tid] = own;
+      }
+      __syncthreads();
+      sr_sort(sh.list, Q.top_k <= 64 ? 64 : SR_THREADS);   // (the zeros of threads without a token stand behind the others)
+      bound = sh.list[Q.top_k - 1];
+      __syncthreads();
+    }
+    sr_each(row, V, [&](float l, int i) {
+      if (!(l > -INFINITY)) return;
+      const unsigned long long key = sr_key(l, i);
+      if (key < bound) return;
+      const int to = atomicAdd(&sh.found, 1);
+      if (to < SR_LIST) sh.list[to] = key;
+    });
+  } else {
+    // masses over equal parts of [lmax - range, lmax]; what weighs less than 2^-66 is in the last part
+    const float span = R.lmax - lmin, most = (float)(66.0 / R.c), range = fminf(span, most);
+    const float inv = range > 0.f && range < INFINITY ? (SR_BINS - 1) / range : 0.f;
+    auto part = [&](float l) __attribute__((always_inline)) { return l == R.lmax ? 0 : (int)fminf((R.lmax - l) * inv, (float)(SR_BINS - 1)); };
+    for (int i = tid; i < SR_BINS; i += SR_THREADS) sh.hist[i] = 0ull;
+    __syncthreads();
+    unsigned mine = 0;
+    sr_each(row, V, [&](float l, int) {
+      const double x = R.log2w(l);
+      if (!R.counts(l, x)) return;
+      ++mine;
+      atomicAdd(&sh.hist[part(l)], R.mass(x));
+    });
+    __syncthreads();
+    const unsigned long long h0 = sh.hist[2 * tid], h1 = sh.hist[2 * tid + 1];
+    unsigned long long total;
+    const unsigned long long before = sr_scan(h0 + h1, sh.wave, total);
+    if (cut_m) {                                           // the parts in which w = min_p can lie
+      const double l = (double)R.lmax + log2((double)Q.min_p) / R.c, off = 1e-6 * (fabs(l) + fabs((double)R.lmax));
+      const int a = part((float)(l + off)), b = part((float)(l - off));
+      if (tid == 0) { sh.c1 = min(a, b); sh.c2 = max(a, b); }
+    }
+    // the first part at which the sum reaches x: f(part, sum before it, sum through it)
+    auto at = [&](unsigned long long x, auto f) __attribute__((always_inline)) {
+      if (before < x && x <= before + h0) f(2 * tid, before, before + h0);
+      if (before + h0 < x && x <= before + h0 + h1) f(2 * tid + 1, before + h0, before + h0 + h1);
+    };
+    __syncthreads();
+    if (cut_p) {
+      const int c1 = sh.c1, c2 = sh.c2;
+      __syncthreads();
+      at(sr_reach(Q.top_p, total), [&](int i, unsigned long long, unsigned long long) {
+        if (!cut_m || i < c1) { sh.c1 = i; sh.c2 = i; }
+        else if (i <= c2) sh.c2 = c2;
+      });
+      __syncthreads();
+    }
+    const bool cut = cut_p || cut_m;
+    // sums before c1 and through c2: what is kept lies between
+    if (cut) {
+      const int c1 = sh.c1, c2 = sh.c2;
+      if (2 * tid == c1) sh.base_c = before;
+      if (2 * tid + 1 == c1) sh.base_c = before + h0;
+      if (2 * tid == c2) sh.total = before + h0;
+      if (2 * tid + 1 == c2) sh.total = before + h0 + h1;
+    } else if (tid == 0) {
+      sh.base_c = sh.total = total;
+      sh.c1 = sh.c2 = SR_BINS;
+    }
+    __syncthreads();
+    const unsigned long long least = sh.base_c, largest = sh.total;
+    at(least > 0 ? sr_pass(Q.u, least) + 1 : 1ull, [&](int i, unsigned long long b, unsigned long long) { sh.d1 = i; sh.base_d = b; });
+    at(sr_pass(Q.u, largest) + 1, [&](int i, unsigned long long, unsigned long long) { sh.d2 = i; });
+    __syncthreads();
+    const int c1 = sh.c1, c2 = sh.c2, d1 = sh.d1, d2 = sh.d2;
+    unsigned ahead = 0;                                    // tokens before c1
+    sr_each(row, V, [&](float l, int i) {
+      if (!(l > -INFINITY)) return;
+      const int b = part(l);
+      ahead += b < c1;
+      if (!((b >= c1 && b <= c2) || (b >= d1 && b <= d2))) return;
+      const int to = atomicAdd(&sh.found, 1);
+      if (to < SR_LIST) sh.list[to] = sr_key(l, i);
+    });
+    if (!cut) ahead = mine;
+#pragma unroll
+    for (int d = 32; d > 0; d >>= 1) ahead += (unsigned)__shfl_xor((int)ahead, d, 64);
+    if ((tid & 63) == 0) sh.count[tid >> 6] = ahead;
+    if (tid == 0) sh.total = total;
+  }
+  __syncthreads();
+  const int n = sh.found;
+  if (n > SR_LIST) return false;
+  sr_sort(sh.list, n);
+
+  // The list in order, four tokens a thread: running sums.  by parts: the draw's tokens come first, then (or among them) the cuts'; sums start at the parts' own.
+  const bool lists_all = whole || by_prefix;
+  const float span = R.lmax - lmin, most = (float)(66.0 / R.c), range = fminf(span, most);
+  const float inv = range > 0.f && range < INFINITY ? (SR_BINS - 1) / range : 0.f;
+  const int c1 = sh.c1, d2 = sh.d2;
+  const bool apart = !lists_all && d2 + 1 < c1;            // the cuts' parts do not touch the draw's
+  const int limit = Q.top_k > 0 ? Q.top_k : SR_LIST;
+  float value[4];
+  unsigned long long w[4], sum = 0, in_d = 0;
+  int cnt = 0, in_c = 0;
+  bool ok[4], c_part[4], heavy[4];
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    const int i = 4 * tid + e;
+    const unsigned long long key = i < n ? sh.list[i] : 0ull;
+    value[e] = sr_value((uint32_t)(key >> 32));
+    const double x = R.log2w(value[e]);
+    ok[e] = i < n && (!lists_all || i < limit) && R.counts(value[e], x);
+    w[e] = ok[e] ? R.mass(x) : 0ull;
+    heavy[e] = ok[e] && (!cut_m || R.power(fmax(x, -1100.0), 0) >= (double)Q.min_p);
+    const int b = lists_all ? 0 : value[e] == R.lmax ? 0 : (int)fminf((R.lmax - value[e]) * inv, (float)(SR_BINS - 1));
+    c_part[e] = lists_all || b >= c1;
+    sum += w[e];
+    in_d += c_part[e] ? 0ull : w[e];
+    cnt += ok[e];
+    in_c += ok[e] && c_part[e] && heavy[e];
+  }
+  unsigned long long all, all_d = 0;
+  unsigned long long run = sr_scan(sum, sh.wave, all);
+  if (!lists_all) sr_scan(in_d, sh.wave, all_d);
+  const unsigned long long base = lists_all ? 0ull : sh.base_d, jump = apart ? sh.base_c - (sh.base_d + all_d) : 0ull;      // (what lies between the two)
+  const unsigned long long total = lists_all ? all : sh.total;
+  run += base;
+  unsigned long long cum[4];
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    run += w[e];
+    cum[e] = run + (c_part[e] ? jump : 0ull);
+  }
+  // tokens kept: those ahead of the list, and of the list the first (entries of the cuts' parts)
+  unsigned ahead = 0;
+  if (!lists_all)
+    for (int v = 0; v < SR_WAVES; ++v) ahead += sh.count[v];
+  if (tid == 0) { sh.cut_p = 1 << 30; sh.cut_m = 0; sh.first_c = 1 << 30; sh.kept = 0; sh.pick = -1; }
+  __syncthreads();
+  {
+    int first = 1 << 30, counted = 0;
+#pragma unroll
+    for (int e = 3; e >= 0; --e)
+      if (ok[e] && c_part[e]) first = 4 * tid + e;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) counted += ok[e];
+    if (first < 1 << 30) atomicMin(&sh.first_c, first);
+    if (in_c) atomicAdd(&sh.cut_m, in_c);
+    if (counted) atomicAdd(&sh.kept, counted);
+    if (cut_p) {
+      const unsigned long long x = sr_reach(Q.top_p, total);
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        if (ok[e] && c_part[e] && cum[e] >= x && cum[e] - w[e] < x) atomicMin(&sh.cut_p, 4 * tid + e);
+    }
+  }
+  __syncthreads();
+  const bool cut = lists_all || cut_p || cut_m;
+  const int first_c = sh.first_c == 1 << 30 ? 0 : sh.first_c, counted = sh.kept;
+  int last = lists_all ? counted - 1 : cut ? first_c + sh.cut_m - 1 : -1;                     // the last kept entry
+  if (lists_all && cut_m) last = min(last, sh.cut_m - 1);
+  if (cut_p) last = min(last, sh.cut_p);
+  if (tid == 0 && last < first_c) sh.kept_mass = lists_all ? 0ull : sh.base_c;                // (none of the list)
+#pragma unroll
+  for (int e = 0; e < 4; ++e)
+    if (4 * tid + e == last && last >= first_c) sh.kept_mass = cum[e];
+  __syncthreads();
+  const unsigned long long kept_mass = !cut ? total : sh.kept_mass, target = sr_pass(Q.u, kept_mass);
+#pragma unroll
+  for (int e = 0; e < 4; ++e)
+    if (ok[e] && cum[e] > target && cum[e] - w[e] <= target && w[e] > 0) {                     // (one token: sums grow)
+      sh.pick = 4 * tid + e;
+    }
+  __syncthreads();
+  const int pick = sh.pick;
+  if (pick < 0) return false;                              // (cannot be)
+  const unsigned long long key = sh.list[pick];
+  out.token = (int)~(uint32_t)key;
+  out.value = sr_value((uint32_t)(key >> 32));
+  out.kept_mass = kept_mass;
+  out.kept = !cut ? (int)ahead : (int)ahead + max(0, last - first_c + 1);
+  return true;
+}
+
 // grid (rows), a workgroup a row.
 __global__ void __launch_bounds__(SR_THREADS) k_sample_row(SampleArgs P) {
-  __shared__ SrShared sh;
-  __shared__ float wmax[SR_WAVES];
+  __shared__ SrLds lds;
   const int tid = threadIdx.x, seq = blockIdx.x, V = P.vocab;
   const float* row = P.logits + (size_t)seq * P.pitch;
-  float m = -INFINITY;
-  for (int i = tid; i < V; i += SR_THREADS) m = fmaxf(m, row[i]);          // (fmaxf passes over NaN)
-  m = wave_max(m);
-  if ((tid & 63) == 0) wmax[tid >> 6] = m;
+  SrFirst first = {-INFINITY, 0};
+  float lmin = INFINITY;
+  sr_each(row, V, [&](float l, int i) {
+    if (l > first.value) first = {l, i};  // (not NaN)
+    lmin = fminf(lmin, l > -INFINITY ? l : INFINITY);
+  });
+  float m = wave_max(first.value);
+  lmin = -wave_max(-lmin);
+  if ((tid & 63) == 0) { lds.fast.hi[tid >> 6] = m; lds.fast.lo[tid >> 6] = lmin; }
   __syncthreads();
-  for (int w = 0; w < SR_WAVES; ++w) m = fmaxf(m, wmax[w]);
+  for (int w = 0; w < SR_WAVES; ++w) { m = fmaxf(m, lds.fast.hi[w]); lmin = fminf(lmin, lds.fast.lo[w]); }
   if (!(m > -INFINITY)) {                 // nothing to draw from
     if (tid == 0) {
       P.token[seq] = -1;
@@ -143,42 +474,46 @@ __global__ void __launch_bounds__(SR_THREADS) k_sample_row(SampleArgs P) {
     }
     return;
   }
-  const float T = P.temperature ? P.temperature[seq] : 1.f, u = P.uniforms[seq];
+  const float T = P.temperature ? P.temperature[seq] : 1.f;
   const bool greedy = !(T > 0.f);
-  const SrRow R = {m, greedy ? 0.0 : 1.4426950408889634 / (double)T, P.S};
-  const float min_p = P.min_p ? P.min_p[seq] : 0.f, top_p = P.top_p ? P.top_p[seq] : 1.f;
-  const int top_k = greedy ? 1 : P.top_k ? P.top_k[seq] : 0;
-  SrSum all = {0, 0}, heavy = {0, 0};
-  for (int i = tid; i < V; i += SR_THREADS) {
-    const float l = row[i];
-    if (!(l > -INFINITY)) continue;
-    const double x = R.log2w(l);
-    if (!R.counts(l, x)) continue;
-    const SrSum one = {R.mass(x), 1u};
-    all = all + one;
-    if (exp2(x) >= (double)min_p) heavy = heavy + one;
+  const SrRow R = {m, 1.4426950408889634 / (greedy ? 1.0 : (double)T), P.S};
+  SrRules Q = {P.uniforms[seq], P.top_p ? P.top_p[seq] : 1.f, P.min_p ? P.min_p[seq] : 0.f, P.top_k ? max(P.top_k[seq], 0) : 0, greedy};
+  if (greedy || Q.min_p > 1.f || Q.top_p <= 0.f) {                       // the first token
+    Q.top_k = 1;
+    Q.min_p = 0.f;
+    Q.top_p = 1.f;
   }
-  all = sr_block_sum(all, sh);
-  SrSum kept = all;
-  if (top_k > 0 && (unsigned)top_k < all.count) kept = sr_find(row, V, P.index_bits, R, false, (unsigned long long)top_k - 1, sh).through;
-  if (!greedy && top_p < 1.f) {
-    const double want = ceil(fmax((double)top_p, 0.0) * (double)kept.mass);
-    const unsigned long long x = want < 1.0 ? 1ull : (unsigned long long)want;
-    const SrSum p = sr_find(row, V, P.index_bits, R, true, (x < kept.mass ? x : kept.mass) - 1, sh).through;
-    if (p.count < kept.count) kept = p;
+  SrOut out;
+  if (!sr_fast(row, V, R, Q, first, lmin, lds.fast, out)) {
+    __syncthreads();
+    SrSum all = {0, 0}, heavy = {0, 0};
+    for (int i = tid; i < V; i += SR_THREADS) {
+      const float l = row[i];
+      const double x = R.log2w(l);
+      if (!R.counts(l, x)) continue;
+      const SrSum one = {R.mass(x), 1u};
+      all = all + one;
+      if (R.power(fmax(x, -1100.0), 0) >= (double)Q.min_p) heavy = heavy + one;
+    }
+    SrShared& sh = lds.slow;
+    all = sr_block_sum(all, sh);
+    SrSum kept = all;
+    if (Q.top_k > 0 && (unsigned)Q.top_k < all.count) kept = sr_find(row, V, P.index_bits, R, false, (unsigned long long)Q.top_k - 1, sh).through;
+    if (!greedy && Q.top_p < 1.f) {
+      const SrSum p = sr_find(row, V, P.index_bits, R, true, sr_reach(Q.top_p, kept.mass) - 1, sh).through;
+      if (p.count < kept.count) kept = p;
+    }
+    if (!greedy && Q.min_p > 0.f) {
+      heavy = sr_block_sum(heavy, sh);
+      if (heavy.count < kept.count) kept = heavy;
+    }
+    const SrFound f = sr_find(row, V, P.index_bits, R, true, sr_pass(Q.u, kept.mass), sh);
+    out = {f.index, f.value, kept.mass, (int)kept.count};
   }
-  if (!greedy && min_p > 0.f) {
-    heavy = sr_block_sum(heavy, sh);
-    if (heavy.count == 0) heavy = sr_find(row, V, P.index_bits, R, false, 0, sh).through;     // (min_p > 1: the first token)
-    if (heavy.count < kept.count) kept = heavy;
-  }
-  const double want = floor(fmax((double)u, 0.0) * (double)kept.mass);
-  const unsigned long long target = want < (double)kept.mass ? (unsigned long long)want : kept.mass - 1;
-  const SrFound f = sr_find(row, V, P.index_bits, R, true, target < kept.mass ? target : kept.mass - 1, sh);
   if (tid == 0) {
-    P.token[seq] = f.index;
-    if (P.logprob) P.logprob[seq] = (float)(R.log2w(f.value) * 0.6931471805599453 - log(ldexp((double)kept.mass, -P.S)));
-    if (P.kept) P.kept[seq] = (int)kept.count;
+    P.token[seq] = out.token;
+    if (P.logprob) P.logprob[seq] = (float)(R.log2w(out.value) * 0.6931471805599453 - log(ldexp((double)out.kept_mass, -P.S)));
+    if (P.kept) P.kept[seq] = out.kept;
   }
 }
 

@@ -1,7 +1,11 @@
 // Attention of trees of drafted tokens over the paged cache and over the trees themselves (first_op_tree_attn).
 //   o = softmax(scale q K^T) V over the cached positions < len and the nodes that the node's mask names; 0 where there are none.
+//
+// The rows of a workgroup are (node, query head of one KV head) pairs of one sequence, so that the keys and values of a KV head are
+// fetched once for all nodes and all of its query heads.  The keys are cut into splits; a workgroup walks one in tiles, with running maximum and
+// sum, and where there are several splits a second kernel joins them.  Split 0 begins with the tree's own keys.
 #pragma once
-#include "common.h"
+#include "mfma_tiles.h"
 
 namespace first {
 
@@ -13,54 +17,359 @@ struct TreeArgs {
   float* lse;
   int B, N, Hq, Hkv, n_pages, max_pages, words, max_nodes, max_len;
   float scale;
+  int split_keys, splits;                 // keys of a split, splits of max_len
+  float *part, *ml;                       // splits > 1: [split][N * Hq][hd] weighted values, [split][N * Hq][2] maximum (as an exponent of 2) and sum
 };
-constexpr int TREE_PAGE = 16;
+constexpr int TREE_PAGE = 16, TREE_SPLIT_MAX = 8192;
+constexpr int TREE_MAX_NODES = 2048;      // (a sequence's nodes through one descriptor: 2^11 nodes of 2^10 heads of 2^9 bytes)
 
-// grid (nodes, query heads, sequences): a workgroup a row, a wave every fourth key.
-template <typename E, int HD>
-__global__ void __launch_bounds__(WG) k_tree_rows(TreeArgs P) {
-  __shared__ float red[WAVES][HD + 2];
-  constexpr int DL = HD / 64;
-  const int b = blockIdx.z, h = blockIdx.y, i = blockIdx.x, wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+// What the host and the kernels take of the numbers on the device.
+struct TreeSeq { int o0, n, len; };
+__device__ __forceinline__ TreeSeq tree_seq(const TreeArgs& P, int b) {
   const int o0 = max(0, min(P.offs[b], P.N)), n = min(min(P.offs[b + 1], P.N) - o0, P.max_nodes);
-  if (i >= n) return;
-  const int len = max(0, min(min(P.lens[b], P.max_len), P.max_pages * TREE_PAGE)), g = h / (P.Hq / P.Hkv);
-  const size_t page = (size_t)2 * P.Hkv * TREE_PAGE * HD;
-  float q[DL], o[DL] = {}, m = -INFINITY, l = 0.f;
-  for (int e = 0; e < DL; ++e) q[e] = to_f32(reinterpret_cast<const E*>(P.q)[((size_t)(o0 + i) * P.Hq + h) * HD + lane * DL + e]);
-  auto take = [&](const E* kr, const E* vr) {
-    float s = 0.f;
-    for (int e = 0; e < DL; ++e) s = fmaf(q[e], to_f32(kr[lane * DL + e]), s);
-    s = wave_sum(s) * P.scale;
-    const float mn = fmaxf(m, s), c = m == -INFINITY ? 0.f : expf(m - mn), w = expf(s - mn);
-    l = l * c + w;
-    m = mn;
-    for (int e = 0; e < DL; ++e) o[e] = o[e] * c + w * to_f32(vr[lane * DL + e]);
+  return {o0, max(n, 0), (int)max(0ll, min((long long)min(P.lens[b], P.max_len), (long long)P.max_pages * TREE_PAGE))};
+}
+
+// 16 bytes of both operands, multiplied: 8 bf16 of each half of the wave in one product of depth 16, or 4 fp32 in four of depth 2.
+__device__ __forceinline__ void tree_mma(bf16, floatx16_t& acc, u32x4_t a, u32x4_t b) {
+  acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, a), __builtin_bit_cast(bf16x8_t, b), acc, 0, 0, 0);
+}
+__device__ __forceinline__ void tree_mma(float, floatx16_t& acc, u32x4_t a, u32x4_t b) {
+#pragma unroll
+  for (int e = 0; e < 4; ++e) acc = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(a[e]), __uint_as_float(b[e]), acc, 0, 0, 0);
+}
+
+// A tile of TK keys: rows of RB bytes, their 16-byte chunks permuted by row so that the reads below spread over all banks.  Keys are read a
+// chunk of 32 rows at a time, values of four keys by 16 dims (bf16, transposed on the way), or of two keys by 32 dims (fp32).
+template <int RB> __device__ __forceinline__ int tree_kslot(int row, int c) { return RB == 128 ? c ^ ((row >> 1) & 7) : c ^ (row & 15); }
+template <typename E, int RB> __device__ __forceinline__ int tree_vslot(int row, int c) {
+  if (sizeof(E) == 4) return c ^ (((row >> 2) & 1) * 8);
+  return RB == 128 ? c ^ (((row >> 1) & 3) * 2) : c ^ ((row & 7) * 2);
+}
+
+typedef short tree_s4_t __attribute__((ext_vector_type(4)));
+typedef __attribute__((address_space(3))) tree_s4_t* tree_lds4_t;
+
+// QG groups of 32 rows x KH shares of a tile's keys (NS blocks of 32 each); S tiles in the ring.  grid (KV heads x blocks of 32 QG rows, splits, B)
+//
+// Everything is transposed, so that a lane owns ONE row of the result (column of the products): S^T = K Q^T and O^T = V^T P^T with the weights
+// straight from the accumulators of S^T, bf16 ones split into two parts (with one part their rounding would be as large as that of the
+// output).  The values' operand, eight keys of one dim, comes out of LDS through transposed reads.  Accumulators of the 32x32 MFMA: lane l
+// holds column l % 32, register r holds row 8 (r / 4) + 4 (l / 32) + r % 4.
+template <typename E, int HD, int QG, int KH, int NS, int S>
+__global__ void __launch_bounds__(QG * KH * 64, QG == 1 ? 1 : 2) k_tree_attn(TreeArgs P) {
+  constexpr int NW = QG * KH, TK = KH * NS * 32, RB = HD * (int)sizeof(E), CPR = RB / 16, RPL = 64 / CPR, NI = TK / RPL / NW;
+  constexpr int KB = TK * RB, STG = 2 * KB, KS = RB / 32, DT = HD / 32;
+  static_assert(TK % (RPL * NW) == 0 && NI >= 1 && TK % TREE_PAGE == 0, "whole loads");
+  static_assert((size_t)QG * (KH - 1) * (16 * DT + 2) * 256 <= (size_t)S * STG, "partial results of the shares fit the ring");
+  extern __shared__ __align__(16) char tree_smem[];
+  __shared__ int pages[TREE_SPLIT_MAX / TREE_PAGE];
+  const uint32_t lds0 = (uint32_t)(size_t)(__attribute__((address_space(3))) void*)tree_smem;
+  const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)), lane = threadIdx.x & 63, col = lane & 31, gl = lane >> 5;
+  const int b = blockIdx.z, split = blockIdx.y, g = blockIdx.x % P.Hkv, G = P.Hq / P.Hkv;
+  const TreeSeq q = tree_seq(P, b);
+  const int rows = q.n * G, row0 = blockIdx.x / P.Hkv * (32 * QG);
+  const int k_lo = split * P.split_keys, k_hi = min(q.len, k_lo + P.split_keys);
+  if (row0 >= rows || (split > 0 && k_lo >= q.len)) return;
+  const int n_tree = split == 0 ? (q.n + TK - 1) / TK : 0, n_tiles = n_tree + max(0, k_hi - k_lo + TK - 1) / TK;
+  const int n_pg = max(0, k_hi - k_lo + TREE_PAGE - 1) / TREE_PAGE;
+  bool hole = false;
+  for (int i = threadIdx.x; i < n_pg; i += NW * 64) {
+    const int id = P.table[(size_t)b * P.max_pages + k_lo / TREE_PAGE + i];
+    const bool ok = id >= 0 && id < P.n_pages;
+    pages[i] = ok ? id : -1;
+    hole |= !ok;
+  }
+  const bool holes = __syncthreads_or(hole);
+
+  const int qg = wave % QG, kh = wave / QG, ri = row0 + qg * 32 + col, rc = min(ri, rows - 1);
+  const int node = rc / G, head = g * G + rc % G;
+  const size_t orow = (size_t)(q.o0 + node) * P.Hq + head;
+  const bool live = row0 + qg * 32 < rows;
+  u32x4_t Q[KS];
+  {
+    const char* x = reinterpret_cast<const char*>(P.q) + orow * RB + gl * 16;
+#pragma unroll
+    for (int s = 0; s < KS; ++s) Q[s] = *reinterpret_cast<const u32x4_t*>(x + s * 32);
+  }
+  // what this lane fetches of a tile's keys and values, and where that lies in a page
+  const int lrow = lane / CPR;
+  uint32_t ck[NI], cv[NI];
+#pragma unroll
+  for (int i = 0; i < NI; ++i) {
+    const int row = (wave * NI + i) * RPL + lrow;
+    ck[i] = tree_kslot<RB>(row, lane % CPR) * 16;
+    cv[i] = tree_vslot<E, RB>(row, lane % CPR) * 16;
+  }
+  const size_t page_bytes = (size_t)2 * P.Hkv * TREE_PAGE * RB;
+  auto issue = [&](int t, int slot) __attribute__((always_inline)) {
+    const uint32_t at = (uint32_t)__builtin_amdgcn_readfirstlane((int)(lds0 + (uint32_t)slot * STG + (uint32_t)wave * NI * 1024));
+    if (t < n_tree) {
+      const uint32_t pitch = (uint32_t)P.Hkv * RB, bytes = (uint32_t)(q.n - 1) * pitch + RB;
+      const size_t first = ((size_t)q.o0 * P.Hkv + g) * RB;
+      const i32x4_t rk = pg_rsrc(reinterpret_cast<const char*>(P.k) + first, bytes), rv = pg_rsrc(reinterpret_cast<const char*>(P.v) + first, bytes);
+#pragma unroll
+      for (int i = 0; i < NI; ++i) {
+        const uint32_t j = t * TK + (wave * NI + i) * RPL + lrow, off = j < (uint32_t)q.n ? j * pitch : 0x7ffffe00u;   // (no such node: zeros)
+        pg_load_lds(at + i * 1024, off + ck[i], rk, 0u);
+        pg_load_lds(at + KB + i * 1024, off + cv[i], rv, 0u);
+      }
+      return;
+    }
+    const int k0 = (t - n_tree) * TK;                      // from the split's first key
+#pragma unroll
+    for (int i = 0; i < NI; ++i) {
+      const int r = (wave * NI + i) * RPL, pg = (k0 + r) / TREE_PAGE, id = pg < n_pg ? __builtin_amdgcn_readfirstlane(pages[pg]) : -1;
+      const i32x4_t rs = pg_rsrc(reinterpret_cast<const char*>(P.pool) + (size_t)max(id, 0) * page_bytes, id >= 0 ? (uint32_t)page_bytes : 0u);
+      const uint32_t off = k_lo + k0 + r + lrow < k_hi ? (uint32_t)(g * TREE_PAGE + r % TREE_PAGE + lrow) * RB : 0x7ff00000u;   // (past the end: zeros)
+      pg_load_lds(at + i * 1024, off + ck[i], rs, 0u);
+      pg_load_lds(at + KB + i * 1024, off + (uint32_t)P.Hkv * TREE_PAGE * RB + cv[i], rs, 0u);
+    }
   };
-  for (int j = wave; j < len; j += WAVES) {
-    const int id = P.table[(size_t)b * P.max_pages + j / TREE_PAGE];
-    if (id < 0 || id >= P.n_pages) continue;
-    const E* kr = reinterpret_cast<const E*>(P.pool) + (size_t)id * page + ((size_t)g * TREE_PAGE + j % TREE_PAGE) * HD;
-    take(kr, kr + (size_t)P.Hkv * TREE_PAGE * HD);
+
+  floatx16_t O[DT];
+#pragma unroll
+  for (int t = 0; t < DT; ++t)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) O[t][r] = 0.f;
+  float m = -INFINITY, l = 0.f;
+  const float sl = P.scale * LOG2E;
+  // bits of the 32 nodes from j0 on that this lane's row sees, moved so that bit 8 (r / 4) + r % 4 is that of register r
+  auto seen = [&](int j0) __attribute__((always_inline)) {
+    const int left = q.n - j0;
+    uint32_t w = left >= 32 ? ~0u : left <= 0 ? 0u : (1u << left) - 1u;
+    if (left > 0) {
+      if (P.mask != nullptr) w &= (uint32_t)(P.mask[(size_t)(q.o0 + node) * P.words + j0 / 64] >> (j0 % 64));
+      else w &= node - j0 >= 31 ? ~0u : node < j0 ? 0u : (2u << (node - j0)) - 1u;
+    }
+    return w >> (4 * gl);
+  };
+#pragma unroll
+  for (int t = 0; t < S - 1; ++t)
+    if (t < n_tiles) issue(t, t);
+  int slot = 0;
+  for (int t = 0; t < n_tiles; ++t) {
+    if (t + S - 2 < n_tiles) pg_wait<2 * NI * (S - 2)>(); else pg_wait<0>();
+    lds_barrier();
+    if (t + S - 1 < n_tiles) issue(t + S - 1, slot == 0 ? S - 1 : slot - 1);
+    const char* sk = tree_smem + slot * STG;
+    const char* sv = sk + KB;
+    slot = slot + 1 == S ? 0 : slot + 1;
+    const bool tree = t < n_tree;
+    const int k0 = tree ? t * TK + kh * NS * 32 : (t - n_tree) * TK + kh * NS * 32;      // this wave's first key
+    if (!live || k0 >= (tree ? q.n : k_hi - k_lo)) continue;
+    floatx16_t W[NS];
+#pragma unroll
+    for (int u = 0; u < NS; ++u)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) W[u][r] = 0.f;
+#pragma unroll
+    for (int s = 0; s < KS; ++s)
+#pragma unroll
+      for (int u = 0; u < NS; ++u) {
+        const int row = (kh * NS + u) * 32 + col;
+        tree_mma(E{}, W[u], *reinterpret_cast<const u32x4_t*>(sk + row * RB + tree_kslot<RB>(row, 2 * s + gl) * 16), Q[s]);
+      }
+#pragma unroll
+    for (int u = 0; u < NS; ++u)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) W[u][r] *= sl;
+    if (tree || k0 + NS * 32 > k_hi - k_lo || holes) {
+#pragma unroll
+      for (int u = 0; u < NS; ++u) {
+        uint32_t w;
+        if (tree) {
+          w = seen(k0 + 32 * u);
+        } else {
+          const int at = k0 + 32 * u, left = k_hi - k_lo - at, pg = at / TREE_PAGE;
+          w = left >= 32 ? ~0u : left <= 0 ? 0u : (1u << left) - 1u;
+          if (holes) w &= (pg < n_pg && pages[pg] >= 0 ? 0xffffu : 0u) | (pg + 1 < n_pg && pages[pg + 1] >= 0 ? 0xffff0000u : 0u);
+          w >>= 4 * gl;
+        }
+#pragma unroll
+        for (int r = 0; r < 16; ++r) W[u][r] = w >> (8 * (r >> 2) + (r & 3)) & 1u ? W[u][r] : -INFINITY;
+      }
+    }
+    float mt = W[0][0];
+#pragma unroll
+    for (int u = 0; u < NS; ++u)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) mt = fmaxf(mt, W[u][r]);
+    float ma, mb;
+    both_halves(mt, ma, mb);
+    const float mn = fmaxf(m, fmaxf(ma, mb)), mu = mn == -INFINITY ? 0.f : mn;           // (nothing seen yet: weights of 0)
+    if (__any(mn > m)) {
+      const float corr = __builtin_amdgcn_exp2f(m - mu);
+      l *= corr;
+#pragma unroll
+      for (int d = 0; d < DT; ++d)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) O[d][r] *= corr;
+      m = mn;
+    }
+    float ls[4] = {0.f, 0.f, 0.f, 0.f};                    // the tile's sum first: a long cache's l is thousands of terms
+#pragma unroll
+    for (int u = 0; u < NS; ++u)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) { W[u][r] = __builtin_amdgcn_exp2f(W[u][r] - mu); ls[r & 3] += W[u][r]; }
+    l += (ls[0] + ls[1]) + (ls[2] + ls[3]);
+    if constexpr (sizeof(E) == 2) {
+      // k-step s2 of a block: keys 16 s2 + 4 gl + 0..3 and 8 more, the rows of registers 8 s2 .. 8 s2 + 7
+#pragma unroll
+      for (int s2 = 0; s2 < 2 * NS; ++s2) {
+        union { uint32_t w[4]; u32x4_t x; } ph, pl;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) split_pair(W[s2 / 2][8 * (s2 & 1) + 2 * e], W[s2 / 2][8 * (s2 & 1) + 2 * e + 1], ph.w[e], pl.w[e]);
+        const int row = kh * NS * 32 + 16 * s2 + 4 * gl + ((lane & 15) >> 2);
+        u32x4_t vf[DT];
+#pragma unroll
+        for (int d = 0; d < DT; ++d) {
+          const int chunk = 4 * d + 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1);
+          union { tree_s4_t s[2]; u32x4_t x; } f;
+#pragma unroll
+          for (int e = 0; e < 2; ++e)
+            f.s[e] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((tree_lds4_t)(sv + (row + 8 * e) * RB + tree_vslot<E, RB>(row + 8 * e, chunk) * 16 + (lane & 1) * 8));
+          vf[d] = f.x;
+        }
+#pragma unroll
+        for (int d = 0; d < DT; ++d) tree_mma(E{}, O[d], vf[d], pl.x);
+#pragma unroll
+        for (int d = 0; d < DT; ++d) tree_mma(E{}, O[d], vf[d], ph.x);
+      }
+    } else {
+#pragma unroll
+      for (int u = 0; u < NS; ++u)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+          const int row = (kh * NS + u) * 32 + 8 * (r >> 2) + 4 * gl + (r & 3);
+#pragma unroll
+          for (int d = 0; d < DT; ++d)
+            O[d] = __builtin_amdgcn_mfma_f32_32x32x2f32(*reinterpret_cast<const float*>(sv + row * RB + tree_vslot<E, RB>(row, 8 * d + (col >> 2)) * 16 + (col & 3) * 4),
+                                                        W[u][r], O[d], 0, 0, 0);
+        }
+    }
+    if (tree && (t + 1) * TK + kh * NS * 32 >= q.n) {       // the wave's last keys of the tree
+      // The products above take nodes that a row does not see times 0: an infinity or NaN there must not reach the row.  Where any is about (rare),
+      // the wave's share of the tree again, a key at a time and only the seen ones.
+      bool odd = false;
+#pragma unroll
+      for (int d = 0; d < DT; ++d)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) odd |= !(fabsf(O[d][r]) < INFINITY);
+      if (__any(odd)) {
+        m = -INFINITY; l = 0.f;
+#pragma unroll
+        for (int d = 0; d < DT; ++d)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) O[d][r] = 0.f;
+        const E* qr = reinterpret_cast<const E*>(P.q) + orow * HD;
+        for (int j = 0; j < q.n; ++j) {
+          if (j / (NS * 32) % KH != kh) continue;
+          const bool mine = P.mask != nullptr ? P.mask[(size_t)(q.o0 + node) * P.words + j / 64] >> (j % 64) & 1 : j <= node;
+          if (!mine) continue;
+          const size_t at = ((size_t)(q.o0 + j) * P.Hkv + g) * HD;
+          const E *kr = reinterpret_cast<const E*>(P.k) + at, *vr = reinterpret_cast<const E*>(P.v) + at;
+          float s = 0.f;
+          for (int d = 0; d < HD; ++d) s = fmaf(to_f32(qr[d]), to_f32(kr[d]), s);
+          s *= sl;
+          const float top = fmaxf(m, s), use = top == -INFINITY ? 0.f : top, c = __builtin_amdgcn_exp2f(m - use), w = __builtin_amdgcn_exp2f(s - use);
+          m = top;
+          l = l * c + (gl == 0 ? w : 0.f);                 // (both halves of the wave hold the row, and add their sums at the end)
+#pragma unroll
+          for (int d = 0; d < DT; ++d)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) O[d][r] = fmaf(w, to_f32(vr[32 * d + 8 * (r >> 2) + 4 * gl + (r & 3)]), O[d][r] * c);
+        }
+      }
+    }
   }
-  for (int j = wave; j < n; j += WAVES) {
-    if (P.mask ? !(P.mask[(size_t)(o0 + i) * P.words + j / 64] >> (j % 64) & 1) : j > i) continue;
-    const size_t at = ((size_t)(o0 + j) * P.Hkv + g) * HD;
-    take(reinterpret_cast<const E*>(P.k) + at, reinterpret_cast<const E*>(P.v) + at);
+  float la, lb;
+  both_halves(l, la, lb);
+  l = la + lb;
+  if constexpr (KH > 1) {                                  // the shares of the keys meet in LDS
+    float* ex = reinterpret_cast<float*>(tree_smem) + lane;
+    constexpr int REC = (16 * DT + 2) * 64;
+    lds_barrier();
+    if (kh > 0) {
+      float* to = ex + ((kh - 1) * QG + qg) * REC;
+#pragma unroll
+      for (int d = 0; d < DT; ++d)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) to[(d * 16 + r) * 64] = O[d][r];
+      to[16 * DT * 64] = m; to[(16 * DT + 1) * 64] = l;
+    }
+    lds_barrier();
+    if (kh > 0) return;
+#pragma unroll
+    for (int w = 1; w < KH; ++w) {
+      const float* from = ex + ((w - 1) * QG + qg) * REC;
+      const float m2 = from[16 * DT * 64], l2 = from[(16 * DT + 1) * 64], top = fmaxf(m, m2), use = top == -INFINITY ? 0.f : top;
+      const float c1 = __builtin_amdgcn_exp2f(m - use), c2 = __builtin_amdgcn_exp2f(m2 - use);
+      m = top;
+      l = l * c1 + l2 * c2;
+#pragma unroll
+      for (int d = 0; d < DT; ++d)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) O[d][r] = O[d][r] * c1 + from[(d * 16 + r) * 64] * c2;
+    }
   }
-  for (int e = 0; e < DL; ++e) red[wave][lane * DL + e] = o[e];
-  if (lane == 0) { red[wave][HD] = m; red[wave][HD + 1] = l; }
-  __syncthreads();
-  float M = -INFINITY, L = 0.f;
-  for (int w = 0; w < WAVES; ++w) M = fmaxf(M, red[w][HD]);
-  for (int w = 0; w < WAVES; ++w) L += red[w][HD + 1] > 0.f ? red[w][HD + 1] * expf(red[w][HD] - M) : 0.f;
-  for (int d = threadIdx.x; d < HD; d += WG) {
-    float s = 0.f;
-    for (int w = 0; w < WAVES; ++w)
-      if (red[w][HD + 1] > 0.f) s += red[w][d] * expf(red[w][HD] - M);
-    reinterpret_cast<E*>(P.out)[((size_t)(o0 + i) * P.Hq + h) * HD + d] = from_f32<E>(L > 0.f ? s / L : 0.f);
+  if (ri >= rows) return;
+  const bool whole = P.splits == 1;
+  const float inv = !whole ? 1.f : l > 0.f || l != l ? 1.0f / l : 0.f;
+  if (gl == 0) {
+    if (!whole) *reinterpret_cast<float2*>(P.ml + ((size_t)split * P.N * P.Hq + orow) * 2) = make_float2(m, l);
+    else if (P.lse != nullptr) P.lse[orow] = l == 0.f ? -INFINITY : (m + log2f(l)) * (1.f / LOG2E);
   }
-  if (threadIdx.x == 0 && P.lse) P.lse[(size_t)(o0 + i) * P.Hq + h] = L > 0.f ? M + logf(L) : -INFINITY;
+#pragma unroll
+  for (int d = 0; d < DT; ++d)
+#pragma unroll
+    for (int rr = 0; rr < 4; ++rr) {
+      const int dim = 32 * d + 8 * rr + 4 * gl;
+      const float4 o = make_float4(O[d][4 * rr] * inv, O[d][4 * rr + 1] * inv, O[d][4 * rr + 2] * inv, O[d][4 * rr + 3] * inv);
+      if (!whole) *reinterpret_cast<float4*>(P.part + ((size_t)split * P.N * P.Hq + orow) * HD + dim) = o;
+      else if constexpr (sizeof(E) == 2) *reinterpret_cast<uint2*>(reinterpret_cast<bf16*>(P.out) + orow * HD + dim) = make_uint2(pk_bf16(o.x, o.y), pk_bf16(o.z, o.w));
+      else *reinterpret_cast<float4*>(reinterpret_cast<float*>(P.out) + orow * HD + dim) = o;
+    }
+}
+
+// Joins the splits of a sequence: grid (rows / 4, B), a wave a row, lane: dims lane * HD / 64 ..  The splits of a row are those that have keys, and the first.
+template <typename E, int HD>
+__global__ void __launch_bounds__(WG) k_tree_join(TreeArgs P) {
+  constexpr int DL = HD / 64;
+  const int b = blockIdx.y, row = blockIdx.x * WAVES + (threadIdx.x >> 6), lane = threadIdx.x & 63;
+  const TreeSeq q = tree_seq(P, b);
+  if (row >= q.n * P.Hq) return;
+  const size_t orow = (size_t)q.o0 * P.Hq + row, all = (size_t)P.N * P.Hq;
+  const int ns = max(1, (q.len + P.split_keys - 1) / P.split_keys);
+  float M = -INFINITY;
+  for (int s = lane; s < ns; s += 64) M = fmaxf(M, P.ml[(s * all + orow) * 2]);
+  M = wave_max(M);
+  const float use = M == -INFINITY ? 0.f : M;
+  float o[DL] = {}, L = 0.f;
+  for (int s0 = 0; s0 < ns; s0 += 4) {                     // four splits requested together
+    float2 ml[4];
+    float x[4][DL];
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      const size_t at = min(s0 + u, ns - 1) * all + orow;
+      ml[u] = *reinterpret_cast<const float2*>(P.ml + at * 2);
+#pragma unroll
+      for (int e = 0; e < DL; ++e) x[u][e] = P.part[at * HD + lane * DL + e];
+    }
+#pragma unroll
+    for (int u = 0; u < 4; ++u)
+      if (s0 + u < ns) {
+        const float c = __builtin_amdgcn_exp2f(ml[u].x - use);
+        L = fmaf(ml[u].y, c, L);
+#pragma unroll
+        for (int e = 0; e < DL; ++e) o[e] = fmaf(x[u][e], c, o[e]);
+      }
+  }
+  const float inv = L > 0.f || L != L ? 1.0f / L : 0.f;
+  E* out = reinterpret_cast<E*>(P.out) + orow * HD + lane * DL;
+#pragma unroll
+  for (int e = 0; e < DL; ++e) out[e] = from_f32<E>(o[e] * inv);
+  if (lane == 0 && P.lse != nullptr) P.lse[orow] = L == 0.f ? -INFINITY : (M + log2f(L)) * (1.f / LOG2E);
 }
 
 }  // namespace first

@@ -17,13 +17,6 @@ namespace first {
 constexpr int PACK_PAD = 128;            // padded rows of a prompt are a multiple of this
 constexpr int FA_TILE = 64;              // keys per tile of kc / vt
 constexpr int FA_WIDE_FROM = 2048;       // prompts of at least this many tokens: 128 queries a workgroup
-constexpr float LOG2E = 1.4426950408889634f;
-
-// x in both halves of the wave -> (value of lane % 32 in the lower half, in the upper half)
-__device__ __forceinline__ void both_halves(float x, float& lower, float& upper) {
-  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
-  lower = __uint_as_float(r[0]); upper = __uint_as_float(r[1]);
-}
 
 // Rotation, splits and cache writes of one head (blockIdx.y: query heads, then key heads, then value heads) for 32 padded rows
 // (blockIdx.x).  Queries leave rotated, scaled by qscale and split; keys and

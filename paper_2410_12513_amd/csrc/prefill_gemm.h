@@ -25,23 +25,6 @@ namespace first {
 
 constexpr int PG_BK = 64;                       // K step that segments are counted in (a tile's own step: 64, or 32 where LDS is short)
 
-// 16 bytes per lane from (descriptor base + voff + soff) to LDS byte lds_off + 16 * lane.  No vector register is written: nothing
-// for the compiler to reuse too early; pg_wait / lds_barrier order it.  The LDS offset travels in m0, as an operand: it is the
-// compiler that writes the register, so it knows (m0 written in the asm text would be a write it knows nothing of).
-typedef int i32x4_t __attribute__((ext_vector_type(4)));
-__device__ __forceinline__ void pg_load_lds(uint32_t lds_off, uint32_t voff, i32x4_t rsrc, uint32_t soff) {
-  asm volatile("s_nop 0\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds" ::"{m0}"(lds_off), "v"(voff), "s"(rsrc), "s"(soff) : "memory");
-}
-__device__ __forceinline__ i32x4_t pg_rsrc(const void* p, uint32_t bytes) {
-  const uint64_t a = reinterpret_cast<uint64_t>(p);
-  i32x4_t r;
-  r[0] = __builtin_amdgcn_readfirstlane((int)(uint32_t)a);
-  r[1] = __builtin_amdgcn_readfirstlane((int)(uint32_t)(a >> 32) & 0xffff);
-  r[2] = __builtin_amdgcn_readfirstlane((int)bytes);
-  r[3] = 0x00020000;
-  return r;
-}
-template <int N> __device__ __forceinline__ void pg_wait() { asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory"); }
 // place of a row's chunk: rows of 128 bytes (two rows are all banks), and of 64 bytes (four are)
 __device__ __forceinline__ int pg_chunk(int row, int chunk) { return chunk ^ ((row >> 1) & 7); }
 template <int BK> __device__ __forceinline__ int pg_place(int row, int chunk) { return BK == 64 ? pg_chunk(row, chunk) : chunk ^ ((row >> 2) & 3); }

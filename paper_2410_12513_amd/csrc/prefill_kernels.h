@@ -1,18 +1,9 @@
 // Prefill kernels: every layer runs on the whole prompt (Section 4.3 item 1), the routers
 // are scored on the stream entering each layer (Section 4.1), KV of all layers is written.
 #pragma once
-#include "common.h"
+#include "mfma_tiles.h"
 
 namespace first {
-
-typedef __attribute__((__vector_size__(8 * sizeof(__bf16)))) __bf16 bf16x8_t;
-typedef __attribute__((__vector_size__(16 * sizeof(float)))) float floatx16_t;
-
-// hi = bf16(x), lo = bf16(x - hi) for a pair
-__device__ __forceinline__ void split_pair(float a, float b, uint32_t& hi, uint32_t& lo) {
-  hi = pk_bf16(a, b);
-  lo = pk_bf16(a - __uint_as_float(hi << 16), b - __uint_as_float(hi & 0xffff0000u));
-}
 
 // Prompts go through the layers in groups, packed row after row.
 // The prompts of one group: rows off[j] - off[0] .. of sequence b0 + j, padded rows from poff[j] - poff[0].

@@ -65,7 +65,7 @@ TREE = dict(q=A16, k=A16, v=A16, pool=A16, table=A16, lens=A16, offs=A16, mask=A
     ({"dtype": 2}, -1, "dtype"), ({"n_q_heads": 7}, -1, "heads"), ({"n_q_heads": 0}, -1, "heads"), ({"n_kv_heads": 0}, -1, "heads"), ({"n_q_heads": 2048}, -1, "heads"),
     ({"head_dim": 96}, -1, "head_dim"), ({"page_tokens": 32}, -1, "16 tokens"), ({"n_pages": -1}, -1, "negative"), ({"scale": float("inf")}, -1, "scale"), ({"mask_words": 0}, -1, "mask_words"),
     ({"q": 0}, -1, "null"), ({"pool": 0}, -1, "null"), ({"table": 0}, -1, "null"), ({"offs": 0}, -1, "null"), ({"out": 0}, -1, "null"), ({"k": A16 + 8}, -1, "aligned"), ({"mask": A16 + 4}, -1, "aligned"),
-    ({"B": -1}, -1, "negative"), ({"N": -1}, -1, "negative"), ({"nodes": -1}, -1, "negative"), ({"length": -1}, -1, "negative"), ({"B": 65536}, -3, "sequences"), ({"nodes": 65}, -1, "mask_words")])
+    ({"B": -1}, -1, "negative"), ({"N": -1}, -1, "negative"), ({"nodes": -1}, -1, "negative"), ({"length": -1}, -1, "negative"), ({"B": 65536}, -3, "sequences"), ({"nodes": 2049, "mask_words": 64}, -3, "2048"), ({"nodes": 65}, -1, "mask_words")])
 def test_tree_attention(lib, change, code, word):
     d = B._TreeAttnDesc(**{**TREE_DESC, **{k: v for k, v in change.items() if k in TREE_DESC}})
     _refused(lib, lib.first_op_tree_attn(None, C.byref(d), *{**TREE, **{k: v for k, v in change.items() if k not in TREE_DESC}}.values()), code, word)
