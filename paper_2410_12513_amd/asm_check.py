@@ -14,6 +14,7 @@ what is in flight along branches (see touched_in_flight); it knows nothing of wh
 but it is exactly the pattern of the faults it guards against.  Needs hipcc only, no GPU."""
 from __future__ import annotations
 
+import functools
 import os
 import re
 import subprocess
@@ -33,6 +34,7 @@ def _regs(tok: str):
     return [int(m.group(1))] if m else []
 
 
+@functools.lru_cache(maxsize=None)
 def assembly() -> str:
     """The device code of the library's sources, one after the other."""
     hipcc = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
@@ -141,6 +143,45 @@ def touched_in_flight(asm: str, keys=KERNELS):
             if not grew:
                 break
     return [found[k] for k in sorted(found)]
+
+
+def _sregs(tok: str):
+    m = re.match(r"s\[(\d+):(\d+)\]", tok)
+    if m:
+        return set(range(int(m.group(1)), int(m.group(2)) + 1))
+    m = re.match(r"s(\d+)$", tok)
+    return {int(m.group(1))} if m else set()
+
+
+def scalars_read_too_early(asm: str, keys=KERNELS, states: int = 5):
+    """[(kernel, line number, instruction, what wrote its scalar)]: memory instructions in inline asm that read a scalar register fewer than
+    `states` wait states after a vector instruction wrote it (v_readlane, v_readfirstlane, v_cmp).  The part does not wait by itself, and the compiler,
+    which keeps the distance for its own instructions, does not see one inside an asm statement."""
+    found = []
+    for fn, body in _functions(asm, keys):
+        before, in_asm = [], False                       # (scalars written, wait states, text), latest last
+        for n, t in body:
+            if t.startswith(";;#ASM"):
+                in_asm = t.startswith(";;#ASMSTART")
+                continue
+            if re.match(r"^\.L\S+:$", t):
+                continue
+            op = t.split()[0]
+            scalars = re.findall(r"s\[\d+:\d+\]|\bs\d+\b", t)
+            if in_asm and re.match(r"(buffer|global|scratch|flat)_", op):
+                used, gap = set().union(*map(_sregs, scalars)) if scalars else set(), 0
+                for wrote, length, text in reversed(before):
+                    if gap >= states:
+                        break
+                    if wrote & used:
+                        found.append((fn, n, t, text))
+                        break
+                    gap += length
+            wrote = set()
+            if op.startswith(("v_readlane", "v_readfirstlane", "v_cmp")) and len(t.split()) > 1:
+                wrote = _sregs(t.split()[1].rstrip(","))
+            before = (before + [(wrote, int(t.split()[1], 0) + 1 if op == "s_nop" else 1, t)])[-states - 1:]
+    return found
 
 
 def kernels_seen(asm: str, keys=KERNELS):

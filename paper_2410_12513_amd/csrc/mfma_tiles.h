@@ -31,6 +31,12 @@ __device__ __forceinline__ i32x4_t pg_rsrc(const void* p, uint32_t bytes) {
   r[3] = 0x00020000;
   return r;
 }
+// The same where the descriptor or the offset may come out of a vector register's lanes (v_readlane, v_readfirstlane) right ahead of the load - a kernel that
+// holds more scalars than there are registers keeps some there.  The part asks for five wait states between such a write and a memory instruction that reads it; the compiler
+// keeps them for its own instructions and does not see one in this text.  (Without them a descriptor's last word was read too early once, and the load faulted.)
+__device__ __forceinline__ void pg_load_lds_any(uint32_t lds_off, uint32_t voff, i32x4_t rsrc, uint32_t soff) {
+  asm volatile("s_nop 4\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds" ::"{m0}"(lds_off), "v"(voff), "s"(rsrc), "s"(soff) : "memory");
+}
 template <int N> __device__ __forceinline__ void pg_wait() { asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory"); }
 
 // x in both halves of the wave -> (value of lane % 32 in the lower half, in the upper half)

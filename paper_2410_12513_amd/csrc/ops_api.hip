@@ -61,7 +61,8 @@ LoraPlan lora_plan(int dtype, int m, int n, int k) {
   const int64_t steps = up((int64_t)k * size_of(dtype), 128) / 128;
   if (m <= LORA_STREAM_ROWS) {
     const int64_t groups = (n + 63) / 64;
-    return {0, (int)std::max<int64_t>(1, std::min<int64_t>({(2 * CUS + groups / 2) / groups, steps / 4, 16}))};
+    const int64_t least = up(steps * 128 * (m <= 16 ? 16 : 32), LORA_A_BYTES) / LORA_A_BYTES;      // (a slice of A has to fit its place in LDS)
+    return {0, (int)std::max(least, std::min((2 * CUS + groups / 2) / groups, steps / 4))};
   }
   LoraPlan best = {64, 1};
   double least = 1e300;
@@ -74,7 +75,8 @@ LoraPlan lora_plan(int dtype, int m, int n, int k) {
   }
   return best;
 }
-int64_t lora_t_bytes(int m, int r) { return up((int64_t)m * up(r, 16) * 4, 256); }
+int lora_rp(int r) { return r <= 16 ? 16 : r <= 32 ? 32 : 64; }
+int64_t lora_t_bytes(int m, int r) { return up((int64_t)m * lora_rp(r) * 4, 256); }
 template <typename E> hipError_t launch_lora(hipStream_t st, LoraArgs& P, const LoraPlan& plan) {
   P.shrink_tiles = (P.m + 15) / 16;
   P.shrink_ways = std::max(1, std::min(16, CUS / P.shrink_tiles));
@@ -83,15 +85,15 @@ template <typename E> hipError_t launch_lora(hipStream_t st, LoraArgs& P, const 
   hipError_t e;
   if (plan.tile == 0) {
     const int grid = helpers + (P.n + 63) / 64 * P.ks;
-    e = P.m <= 16 ? launch<&k_lora_stream<E, 16, 4>>(st, grid, WG, 4 * 4 * 32 * 128, P) : launch<&k_lora_stream<E, 32, 3>>(st, grid, WG, 4 * 3 * 48 * 128, P);
+    e = P.m <= 16 ? launch<&k_lora_stream<E, 16, 6>>(st, grid, WG, LORA_A_BYTES + 4 * 6 * 2048, P) : launch<&k_lora_stream<E, 32, 6>>(st, grid, WG, LORA_A_BYTES + 4 * 6 * 2048, P);
   } else {
     e = launch<&k_lora_shrink<E>>(st, helpers, LORA_SHRINK_WAVES * 64, (size_t)LORA_SHRINK_WAVES * 16 * P.rp * 4, P);
     if (e != hipSuccess) return e;
     P.gm = (P.m + plan.tile - 1) / plan.tile;
     P.gn = (P.n + plan.tile - 1) / plan.tile;
     const int grid = P.gm * P.gn * P.ks;
-    e = plan.tile == 256 ? launch<&k_lora_tile<E, 256, 256, 4, 2, 64, 4>>(st, grid, 512, 4 * 512 * 64, P)
-        : plan.tile == 128 ? launch<&k_lora_tile<E, 128, 128, 2, 2, 128, 4>>(st, grid, 256, 4 * 256 * 128, P)
+    e = plan.tile == 256 ? launch<&k_lora_tile<E, 256, 256, 4, 2, 128, 2>>(st, grid, 512, 2 * 512 * 128, P)
+        : plan.tile == 128 ? launch<&k_lora_tile<E, 128, 128, 4, 2, 128, 4>>(st, grid, 512, 4 * 256 * 128, P)
                            : launch<&k_lora_tile<E, 64, 64, 2, 2, 128, 4>>(st, grid, 256, 4 * 128 * 128, P);
   }
   if (e == hipSuccess && (plan.tile == 0 || P.ks > 1)) e = launch<&k_lora_finish<E>>(st, dim3((P.n + WG - 1) / WG, P.m), WG, 0, P);
@@ -204,7 +206,7 @@ int first_op_gemm_nt_lora(void* hip_stream, int32_t dtype, const void* A, const 
     return refuse(FIRST_ERR_ARG, "first_op_gemm_nt_lora: A, W, La, Lb and the workspace must be on 16 bytes, the others on 4");
   if (workspace_bytes < need) return refuse(FIRST_ERR_CAPACITY, "first_op_gemm_nt_lora: the workspace is smaller than first_op_gemm_nt_lora_workspace says");
   if (m > 1 << 20 || n > 1 << 20 || k > 1 << 20) return refuse(FIRST_ERR_CAPACITY, "first_op_gemm_nt_lora: more than 2^20 rows or columns");
-  LoraArgs P = {A, W, La, Lb, adapter, scale, C, (float*)workspace, (float*)((char*)workspace + lora_t_bytes(m, r)), m, n, k, r, (int)up(r, 16), n_adapters, accumulate != 0};
+  LoraArgs P = {A, W, La, Lb, adapter, scale, C, (float*)workspace, (float*)((char*)workspace + lora_t_bytes(m, r)), m, n, k, r, lora_rp(r), n_adapters, accumulate != 0};
   const LoraPlan plan = lora_plan(dtype, m, n, k);
   const hipStream_t st = stream_of(hip_stream);
   return launched("first_op_gemm_nt_lora", dtype == FIRST_DTYPE_BF16 ? launch_lora<bf16>(st, P, plan) : launch_lora<float>(st, P, plan));

@@ -50,17 +50,18 @@ template <int RB> __device__ __forceinline__ int lora_slot(int row, int c) { ret
 // ---- T ---------------------------------------------------------------------------------------------------------------------
 // A workgroup takes 16 rows and every ways-th of the adapters among them; its waves share K out in steps of 64 bytes a row, and their sums meet in LDS.
 // Rows without an adapter get their zeros from way 0.  red: NW * 16 * rp floats.
-template <typename E, int NW>
+template <typename E, int NW, int NP>     // NP: blocks of 16 ranks, all of them (rp = 16 NP)
 __device__ __forceinline__ void lora_shrink(const LoraArgs& P, int tile, int way, float* red) {
-  constexpr int EPC = 16 / (int)sizeof(E);                 // elements of a chunk
+  constexpr int EPC = 16 / (int)sizeof(E), RP = 16 * NP;   // elements of a chunk
+  constexpr int U = NP == 1 ? 8 : NP == 2 ? 4 : 2;         // steps of a wave requested together
   const int wave = lora_uni((int)(threadIdx.x >> 6)), lane = threadIdx.x & 63, row = lane & 15, quarter = lane >> 4;
-  const int m0 = tile * 16, mr = min(m0 + row, P.m - 1), np = P.rp / 16;
+  const int m0 = tile * 16, mr = min(m0 + row, P.m - 1);
   const int id = P.adapter[mr];
   const bool have = m0 + row < P.m && id >= 0 && id < P.adapters;
   if (way == 0)
-    for (int i = threadIdx.x; i < 16 * P.rp; i += NW * 64) {
-      const int rr = i / P.rp, at = min(m0 + rr, P.m - 1), a = P.adapter[at];
-      if (m0 + rr < P.m && (a < 0 || a >= P.adapters)) P.T[(size_t)at * P.rp + i % P.rp] = 0.f;
+    for (int i = threadIdx.x; i < 16 * RP; i += NW * 64) {
+      const int at = min(m0 + i / RP, P.m - 1), a = P.adapter[at];
+      if (m0 + i / RP < P.m && (a < 0 || a >= P.adapters)) P.T[(size_t)at * RP + i % RP] = 0.f;
     }
   unsigned long long todo = __ballot(have) & 0xffffull;
   const int steps = (P.k + 4 * EPC - 1) / (4 * EPC);
@@ -70,87 +71,87 @@ __device__ __forceinline__ void lora_shrink(const LoraArgs& P, int tile, int way
     const unsigned long long mine = __ballot(have && id == a) & 0xffffull;
     todo &= ~mine;
     if (nth % P.shrink_ways != way) continue;
-    floatx4_t acc[4];
+    floatx4_t acc[NP];
 #pragma unroll
-    for (int p = 0; p < 4; ++p) acc[p] = floatx4_t{0.f, 0.f, 0.f, 0.f};
+    for (int p = 0; p < NP; ++p) acc[p] = floatx4_t{0.f, 0.f, 0.f, 0.f};
     const E* la = reinterpret_cast<const E*>(P.La) + (size_t)a * P.r * P.k;
-    for (int s0 = wave; s0 < steps; s0 += 4 * NW) {        // four steps of a wave requested together
-      u32x4_t xa[4], w[4][4];
+    for (int s0 = wave; s0 < steps; s0 += U * NW) {
+      u32x4_t xa[U], w[U][NP];
 #pragma unroll
-      for (int u = 0; u < 4; ++u) {
+      for (int u = 0; u < U; ++u) {
         const int at = (s0 + u * NW) * 4 * EPC + quarter * EPC;
         const bool ok = at < P.k;
         xa[u] = ok ? *reinterpret_cast<const u32x4_t*>(x + at) : u32x4_t{0, 0, 0, 0};
 #pragma unroll
-        for (int p = 0; p < 4; ++p)
-          if (p < np) w[u][p] = ok && 16 * p + row < P.r ? *reinterpret_cast<const u32x4_t*>(la + (size_t)(16 * p + row) * P.k + at) : u32x4_t{0, 0, 0, 0};
+        for (int p = 0; p < NP; ++p) w[u][p] = ok && 16 * p + row < P.r ? *reinterpret_cast<const u32x4_t*>(la + (size_t)(16 * p + row) * P.k + at) : u32x4_t{0, 0, 0, 0};
       }
 #pragma unroll
-      for (int u = 0; u < 4; ++u)
+      for (int u = 0; u < U; ++u)
 #pragma unroll
-        for (int p = 0; p < 4; ++p)
-          if (p < np) lora_mma16(E{}, acc[p], xa[u], w[u][p]);
+        for (int p = 0; p < NP; ++p) lora_mma16(E{}, acc[p], xa[u], w[u][p]);
     }
     __syncthreads();
 #pragma unroll
-    for (int p = 0; p < 4; ++p)                            // lane: rank 16 p + lane % 16 of rows 4 (lane / 16) ..
-      if (p < np)
+    for (int p = 0; p < NP; ++p)                           // lane: rank 16 p + lane % 16 of rows 4 (lane / 16) ..
 #pragma unroll
-        for (int e = 0; e < 4; ++e) red[(wave * 16 + 4 * quarter + e) * P.rp + 16 * p + row] = acc[p][e];
+      for (int e = 0; e < 4; ++e) red[(wave * 16 + 4 * quarter + e) * RP + 16 * p + row] = acc[p][e];
     __syncthreads();
     const float s = P.scale[a];
-    for (int i = threadIdx.x; i < 16 * P.rp; i += NW * 64) {
-      const int rr = i / P.rp;
+    for (int i = threadIdx.x; i < 16 * RP; i += NW * 64) {
+      const int rr = i / RP;
       if (!(mine >> rr & 1)) continue;
       float t = 0.f;
-      for (int w = 0; w < NW; ++w) t += red[w * 16 * P.rp + i];
-      P.T[(size_t)(m0 + rr) * P.rp + i % P.rp] = i % P.rp < P.r ? t * s : 0.f;
+      for (int w = 0; w < NW; ++w) t += red[w * 16 * RP + i];
+      P.T[(size_t)(m0 + rr) * RP + i % RP] = i % RP < P.r ? t * s : 0.f;
     }
   }
 }
-constexpr int LORA_SHRINK_WAVES = 8;
+template <typename E, int NW> __device__ __forceinline__ void lora_shrink(const LoraArgs& P, int at, float* red) {
+  const int tile = at % P.shrink_tiles, way = at / P.shrink_tiles;
+  if (P.rp == 16) lora_shrink<E, NW, 1>(P, tile, way, red);
+  else if (P.rp == 32) lora_shrink<E, NW, 2>(P, tile, way, red);
+  else lora_shrink<E, NW, 4>(P, tile, way, red);
+}
+constexpr int LORA_SHRINK_WAVES = 16;
 template <typename E> __global__ void __launch_bounds__(LORA_SHRINK_WAVES * 64) k_lora_shrink(LoraArgs P) {
   extern __shared__ __align__(16) char lora_smem[];
-  lora_shrink<E, LORA_SHRINK_WAVES>(P, blockIdx.x % P.shrink_tiles, blockIdx.x / P.shrink_tiles, reinterpret_cast<float*>(lora_smem));
+  lora_shrink<E, LORA_SHRINK_WAVES>(P, blockIdx.x, reinterpret_cast<float*>(lora_smem));
 }
 
 // ---- up to 32 rows ---------------------------------------------------------------------------------------------------------
-// The first shrink_tiles * shrink_ways workgroups form T; the others take 64 rows of W (a wave 16) x a slice of K.  A wave loads its rows and its own copy of
-// A's (they come from L2) straight into a ring of its own: it waits for nobody.  Partial sums [slice][m][n].
-template <typename E, int MR, int S>      // MR: 16 or 32 rows of A
-__global__ void __launch_bounds__(WG) k_lora_stream(LoraArgs P) {
-  constexpr int RB = 128, EPS = RB / (int)sizeof(E), STG = (16 + MR) * RB, NL = (16 + MR) / 8;
+// The first shrink_tiles * shrink_ways workgroups form T; the others take 64 rows of W (a wave 16) x a slice of K.  The slice of A goes into LDS once, and
+// every wave loads its rows of W straight into a ring of its own: it waits for nobody.  Two workgroups a compute unit (80 KB each), 96 KB of W in
+// flight on it.  Partial sums [slice][m][n].
+constexpr int LORA_A_BYTES = 32 * 1024;   // of LDS for the slice of A
+template <typename E, int MR, int S>      // MR: 16 or 32 rows of A; S steps in a wave's ring
+__global__ void __launch_bounds__(WG, 2) k_lora_stream(LoraArgs P) {
+  constexpr int RB = 128, EPS = RB / (int)sizeof(E), STG = 16 * RB;
   extern __shared__ __align__(16) char lora_smem[];
   const int helpers = P.shrink_tiles * P.shrink_ways;
   if ((int)blockIdx.x < helpers) {
-    lora_shrink<E, WAVES>(P, blockIdx.x % P.shrink_tiles, blockIdx.x / P.shrink_tiles, reinterpret_cast<float*>(lora_smem));
+    lora_shrink<E, WAVES>(P, blockIdx.x, reinterpret_cast<float*>(lora_smem));
     return;
   }
   const int id = blockIdx.x - helpers, wave = lora_uni((int)(threadIdx.x >> 6)), lane = threadIdx.x & 63, row = lane & 15, quarter = lane >> 4;
   const int slice = id % P.ks, n0 = (id / P.ks) * 64 + wave * 16;
-  if (n0 >= P.n) return;
-  const uint32_t lds0 = (uint32_t)(size_t)(__attribute__((address_space(3))) void*)lora_smem + wave * S * STG;
-  const char* ring = lora_smem + wave * S * STG;
+  const uint32_t lds0 = (uint32_t)(size_t)(__attribute__((address_space(3))) void*)lora_smem, ring0 = lds0 + LORA_A_BYTES + wave * S * STG;
+  const char* ring = lora_smem + LORA_A_BYTES + wave * S * STG;
   const uint32_t pitch = (uint32_t)P.k * sizeof(E);
-  const i32x4_t rw = pg_rsrc(reinterpret_cast<const char*>(P.W) + (size_t)n0 * pitch, min(16, P.n - n0) * pitch);
+  const int rows_w = max(0, min(16, P.n - n0));
+  const i32x4_t rw = pg_rsrc(reinterpret_cast<const char*>(P.W) + (size_t)min(n0, P.n - 1) * pitch, rows_w * pitch);
   const i32x4_t ra = pg_rsrc(P.A, P.m * pitch);
   const int steps = (P.k + EPS - 1) / EPS, s0 = (int)((long long)steps * slice / P.ks), s1 = (int)((long long)steps * (slice + 1) / P.ks);
   const int tail = (int)(pitch % RB) / 16;                 // chunks of the last step that exist (0: all)
   const int lrow = lane >> 3, lch = lane & 7;
-  uint32_t off[NL];                                        // of this lane's chunk in each load: rows 8 i + lrow of W, then of A
-#pragma unroll
-  for (int i = 0; i < NL; ++i) {
-    const int r = (i < 2 ? i : i - 2) * 8 + lrow;
-    off[i] = r * pitch + lora_slot<RB>(r, lch) * 16;
-  }
+  auto fetch = [&](uint32_t to, i32x4_t rs, int r, int s) __attribute__((always_inline)) {       // rows r .. r + 7 of step s
+    const int chunk = lora_slot<RB>(r + lrow, lch);
+    const uint32_t off = tail != 0 && s == steps - 1 && chunk >= tail ? 0x7ffffff0u : (uint32_t)(r + lrow) * pitch + chunk * 16;
+    pg_load_lds_any((uint32_t)lora_uni((int)to), off, rs, (uint32_t)lora_uni(s * RB));
+  };
+  for (int i = wave; i < (s1 - s0) * (MR / 8); i += WAVES) fetch(lds0 + i * 1024, ra, i % (MR / 8) * 8, s0 + i / (MR / 8));
   auto issue = [&](int s, int slot) __attribute__((always_inline)) {
-    const uint32_t at = (uint32_t)lora_uni((int)(lds0 + slot * STG)), so = (uint32_t)lora_uni(s * RB);
-    const bool cut = tail != 0 && s == steps - 1;
-#pragma unroll
-    for (int i = 0; i < NL; ++i) {
-      const int r = (i < 2 ? i : i - 2) * 8 + lrow;
-      pg_load_lds(at + i * 1024, cut && lora_slot<RB>(r, lch) >= tail ? 0x7ffffff0u : off[i], i < 2 ? rw : ra, so);
-    }
+    fetch(ring0 + slot * STG, rw, 0, s);
+    fetch(ring0 + slot * STG + 1024, rw, 8, s);
   };
   floatx4_t acc[MR / 16];
 #pragma unroll
@@ -158,17 +159,19 @@ __global__ void __launch_bounds__(WG) k_lora_stream(LoraArgs P) {
 #pragma unroll
   for (int s = 0; s < S - 1; ++s)
     if (s0 + s < s1) issue(s0 + s, s);
+  if (s1 - s0 >= S - 1) pg_wait<2 * (S - 1)>(); else pg_wait<0>();      // (A is older)
+  lds_barrier();
   int slot = 0;
   for (int s = s0; s < s1; ++s) {
     // (the slot that is loaded into was read a step ago: its reads have ended, the products took their results)
-    if (s + S - 1 < s1) { issue(s + S - 1, slot == 0 ? S - 1 : slot - 1); pg_wait<NL * (S - 1)>(); } else { pg_wait<0>(); }
-    const char* at = ring + slot * STG;
+    if (s + S - 1 < s1) { issue(s + S - 1, slot == 0 ? S - 1 : slot - 1); pg_wait<2 * (S - 1)>(); } else { pg_wait<0>(); }
+    const char *at = ring + slot * STG, *xa = lora_smem + (s - s0) * MR * RB;
 #pragma unroll
     for (int c = 0; c < 2; ++c) {
       const u32x4_t w = *reinterpret_cast<const u32x4_t*>(at + row * RB + lora_slot<RB>(row, 4 * c + quarter) * 16);
 #pragma unroll
       for (int i = 0; i < MR / 16; ++i)
-        lora_mma16(E{}, acc[i], *reinterpret_cast<const u32x4_t*>(at + (16 + 16 * i + row) * RB + lora_slot<RB>(16 * i + row, 4 * c + quarter) * 16), w);
+        lora_mma16(E{}, acc[i], *reinterpret_cast<const u32x4_t*>(xa + (16 * i + row) * RB + lora_slot<RB>(16 * i + row, 4 * c + quarter) * 16), w);
     }
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
     slot = slot + 1 == S ? 0 : slot + 1;
@@ -221,7 +224,7 @@ template <typename E, int BM, int BN, int WGM, int WGN, int RB, int S>
 __global__ void __launch_bounds__(WGM * WGN * 64, 1) k_lora_tile(LoraArgs P) {
   constexpr int NW = WGM * WGN, TM = BM / WGM, TN = BN / WGN, IM = TM / 32, JN = TN / 32, EPC = 16 / (int)sizeof(E);
   constexpr int RPL = 1024 / RB, CPR = RB / 16, IA = BM / RPL / NW, IB = BN / RPL / NW, NL = IA + IB, STG = (BM + BN) * RB, NKK = RB / 32;
-  static_assert(BM % (RPL * NW) == 0 && BN % (RPL * NW) == 0 && TM % 32 == 0 && TN % 32 == 0 && TM <= 64, "tile shape");
+  static_assert(BM % (RPL * NW) == 0 && BN % (RPL * NW) == 0 && TM % 32 == 0 && TN % 32 == 0 && (TM <= 64 || TM == 128), "tile shape");
   extern __shared__ __align__(16) char lora_smem[];
   const uint32_t lds0 = (uint32_t)(size_t)(__attribute__((address_space(3))) void*)lora_smem;
   const int wave = lora_uni((int)(threadIdx.x >> 6)), lane = threadIdx.x & 63, lr = lane & 31, lg = lane >> 5;
@@ -243,6 +246,9 @@ __global__ void __launch_bounds__(WGM * WGN * 64, 1) k_lora_tile(LoraArgs P) {
   const i32x4_t rb = pg_rsrc(reinterpret_cast<const char*>(P.W) + (size_t)n0 * pitch, rowsB * pitch);
   const int nsteps = (int)((pitch + RB - 1) / RB), tail = (int)(pitch % RB) / 16;
   const int s0 = (int)((long long)nsteps * slice / P.ks), s1 = (int)((long long)nsteps * (slice + 1) / P.ks);
+  // Workgroups of an XCD walk K from the same place, those of different ones from different places: 60 us -> 56 at 250 x 14336 x 4096, where all of them asked for the
+  // same columns of 14336 rows at a time.
+  const int rot = s1 > s0 ? (int)(blockIdx.x % 8) * 5 % (s1 - s0) : 0;
   uint32_t va[IA], vb[IB];
   const int lrow = lane / CPR, lch = lane % CPR;
 #pragma unroll
@@ -250,13 +256,14 @@ __global__ void __launch_bounds__(WGM * WGN * 64, 1) k_lora_tile(LoraArgs P) {
 #pragma unroll
   for (int i = 0; i < IB; ++i) { const int r = (wave * IB + i) * RPL + lrow; vb[i] = r * pitch + lora_slot<RB>(r, lch) * 16; }
   auto issue = [&](int step, int slot) __attribute__((always_inline)) {
+    step = step + rot < s1 ? step + rot : step + rot - (s1 - s0);
     const uint32_t b = (uint32_t)lora_uni((int)(lds0 + (uint32_t)slot * STG)), so = (uint32_t)lora_uni(step * RB);
     const bool cut = tail != 0 && step == nsteps - 1;
     auto off = [&](uint32_t v, int r) __attribute__((always_inline)) { return cut && lora_slot<RB>(r, lch) >= tail ? 0x7ffffff0u : v; };   // (past the row's end: zeros)
 #pragma unroll
-    for (int i = 0; i < IA; ++i) pg_load_lds(b + (wave * IA + i) * 1024, off(va[i], (wave * IA + i) * RPL + lrow), ra, so);
+    for (int i = 0; i < IA; ++i) pg_load_lds_any(b + (wave * IA + i) * 1024, off(va[i], (wave * IA + i) * RPL + lrow), ra, so);
 #pragma unroll
-    for (int i = 0; i < IB; ++i) pg_load_lds(b + BM * RB + (wave * IB + i) * 1024, off(vb[i], (wave * IB + i) * RPL + lrow), rb, so);
+    for (int i = 0; i < IB; ++i) pg_load_lds_any(b + BM * RB + (wave * IB + i) * 1024, off(vb[i], (wave * IB + i) * RPL + lrow), rb, so);
   };
   floatx16_t acc[IM][JN];
 #pragma unroll
@@ -285,46 +292,50 @@ __global__ void __launch_bounds__(WGM * WGN * 64, 1) k_lora_tile(LoraArgs P) {
     if (s0 + s < s1) issue(s0 + s, s);
 
   if (P.ks == 1) {
-    // the second product first, while the first tiles are on their way: the adapters among this wave's rows, one after the other
-    const int mine = m0 + wm + min(lane, TM - 1);
-    const int ad = P.adapter[min(mine, P.m - 1)];
-    unsigned long long todo = __ballot(lane < TM && mine < P.m && ad >= 0 && ad < P.adapters);
-    while (todo != 0) {
-      const int a = __builtin_amdgcn_readlane(ad, __ffsll(todo) - 1);
-      const unsigned long long rows = __ballot(ad == a) & todo;
-      todo &= ~rows;
+    // The second product first, while the first tiles are on their way: the adapters among 64 of this wave's rows, one after the other, all that a step of
+    // two chunks of ranks needs of an adapter requested together.
+    constexpr int H = IM < 2 ? IM : 2;
 #pragma unroll
-      for (int i = 0; i < IM; ++i) {
-        const uint32_t of = (uint32_t)(rows >> (32 * i));
-        if (of == 0) continue;
-        const float* t = P.T + (size_t)min(m0 + wm + 32 * i + lr, P.m - 1) * P.rp;
-        const bool own = of >> lr & 1;
+    for (int h = 0; h < IM / H; ++h) {
+      const int mine = m0 + wm + 64 * h + min(lane, TM - 1), ad = P.adapter[min(mine, P.m - 1)];
+      unsigned long long todo = __ballot(lane < TM && mine < P.m && ad >= 0 && ad < P.adapters);
+      while (todo != 0) {
+        const int a = __builtin_amdgcn_readlane(ad, __ffsll(todo) - 1);
+        const unsigned long long rows = __ballot(ad == a) & todo;
+        todo &= ~rows;
+        const E* const lb = reinterpret_cast<const E*>(P.Lb) + (size_t)a * P.n * P.r;
+        for (int p = 0; p < P.r; p += 2 * EPC) {
+          const int p0 = p + lg * EPC;
+          u32x4_t w[JN], t[H][EPC / 4];
 #pragma unroll
-        for (int j = 0; j < JN; ++j) {
-          const int col = min(n0 + wn + 32 * j + lr, P.n - 1);
-          const E* lb = reinterpret_cast<const E*>(P.Lb) + ((size_t)a * P.n + col) * P.r;
-          floatx16_t d;
-#pragma unroll
-          for (int r = 0; r < 16; ++r) d[r] = 0.f;
-          for (int p0 = lg * EPC; p0 - lg * EPC < P.r; p0 += 2 * EPC) {
-            u32x4_t w;
-            float x[EPC];
+          for (int j = 0; j < JN; ++j) {
+            const E* at = lb + (size_t)min(n0 + wn + 32 * j + lr, P.n - 1) * P.r + p0;
+            w[j] = u32x4_t{0, 0, 0, 0};
             if (P.r % EPC == 0) {
-              w = p0 < P.r ? *reinterpret_cast<const u32x4_t*>(lb + p0) : u32x4_t{0, 0, 0, 0};
+              if (p0 < P.r) w[j] = *reinterpret_cast<const u32x4_t*>(at);
             } else {
               union { E e[EPC]; u32x4_t v; } f;
-              f.v = u32x4_t{0, 0, 0, 0};
+              f.v = w[j];
 #pragma unroll
               for (int e = 0; e < EPC; ++e)
-                if (p0 + e < P.r) f.e[e] = lb[p0 + e];
-              w = f.v;
+                if (p0 + e < P.r) f.e[e] = at[e];
+              w[j] = f.v;
+            }
+          }
+#pragma unroll
+          for (int i = 0; i < H; ++i)
+#pragma unroll
+            for (int e = 0; e < EPC / 4; ++e) {            // (a row of another adapter: zeros; rp is a multiple of two chunks)
+              t[i][e] = u32x4_t{0, 0, 0, 0};
+              if (rows >> (32 * i + lr) & 1) t[i][e] = *reinterpret_cast<const u32x4_t*>(P.T + (size_t)(m0 + wm + 64 * h + 32 * i + lr) * P.rp + p0 + 4 * e);
             }
 #pragma unroll
-            for (int e = 0; e < EPC; ++e) x[e] = own && p0 + e < P.rp ? t[p0 + e] : 0.f;
-            if constexpr (sizeof(E) == 4) {
-              lora_mma32(E{}, d, u32x4_t{__float_as_uint(x[0]), __float_as_uint(x[1]), __float_as_uint(x[2]), __float_as_uint(x[3])}, w);
-            } else {
-              u32x4_t part[3];
+          for (int i = 0; i < H; ++i) {
+            u32x4_t part[3];
+            if constexpr (sizeof(E) == 2) {
+              float x[EPC];
+#pragma unroll
+              for (int e = 0; e < EPC; ++e) x[e] = __uint_as_float(t[i][e / 4][e % 4]);
 #pragma unroll
               for (int q = 0; q < 3; ++q)
 #pragma unroll
@@ -332,12 +343,23 @@ __global__ void __launch_bounds__(WGM * WGN * 64, 1) k_lora_tile(LoraArgs P) {
                   part[q][e] = pk_bf16(x[2 * e], x[2 * e + 1]);
                   x[2 * e] -= __uint_as_float(part[q][e] << 16); x[2 * e + 1] -= __uint_as_float(part[q][e] & 0xffff0000u);
                 }
+            }
+            const uint32_t of = (uint32_t)(rows >> (32 * i)) >> (4 * lg);
 #pragma unroll
-              for (int q = 2; q >= 0; --q) lora_mma32(E{}, d, part[q], w);
+            for (int j = 0; j < JN; ++j) {
+              floatx16_t d;
+#pragma unroll
+              for (int r = 0; r < 16; ++r) d[r] = 0.f;
+              if constexpr (sizeof(E) == 2) {
+#pragma unroll
+                for (int q = 2; q >= 0; --q) lora_mma32(E{}, d, part[q], w[j]);
+              } else {
+                lora_mma32(E{}, d, t[i][0], w[j]);
+              }
+#pragma unroll
+              for (int r = 0; r < 16; ++r) acc[H * h + i][j][r] += of >> (8 * (r >> 2) + (r & 3)) & 1 ? d[r] : 0.f;
             }
           }
-#pragma unroll
-          for (int r = 0; r < 16; ++r) acc[i][j][r] += of >> (8 * (r >> 2) + 4 * lg + (r & 3)) & 1 ? d[r] : 0.f;
         }
       }
     }

@@ -47,27 +47,32 @@ struct SrRow {                            // what a row's weights are made of
   __device__ __forceinline__ double log2w(float l) const { return l == lmax ? 0.0 : ((double)l - (double)lmax) * c; }
   // tokens that count at all: the weight is not 0 in 64 bits
   __device__ __forceinline__ bool counts(float l, double x) const { return l > -INFINITY && x > -1074.5; }
-  // 2^x 2^e: the power series of 2^f, f the rest of x to the nearest whole number, to f^11 (6e-15 at f = 1/2)
-  __device__ __forceinline__ double power(double x, int e) const {
-    const double n = rint(x), f = x - n;
-    double p = 4.4455382718708115e-10;
-    p = fma(p, f, 7.0549116208011233e-9);
-    p = fma(p, f, 1.0178086009239700e-7);
-    p = fma(p, f, 1.3215486790144310e-6);
-    p = fma(p, f, 1.5252733804059840e-5);
-    p = fma(p, f, 1.5403530393381610e-4);
-    p = fma(p, f, 1.3333558146428443e-3);
-    p = fma(p, f, 9.6181291076284772e-3);
-    p = fma(p, f, 5.5504108664821580e-2);
-    p = fma(p, f, 2.4022650695910071e-1);
-    p = fma(p, f, 6.9314718055994531e-1);
+  // 2^t.  f, the rest of t to the nearest whole number: 2^f = 1 + f q(f), q of degree 9 through the Chebyshev points of [-1/2, 1/2] (6e-16)
+  __device__ __forceinline__ static double power(double t) {
+    const double n = rint(t), f = t - n;
+    double p = 7.070977963327673e-09;
+    p = fma(p, f, 1.0205905547945269e-07);
+    p = fma(p, f, 1.3215451634133493e-06);
+    p = fma(p, f, 1.5252672924230416e-05);
+    p = fma(p, f, 0.00015403530424769424);
+    p = fma(p, f, 0.001333355820079545);
+    p = fma(p, f, 0.00961812910761868);
+    p = fma(p, f, 0.05550410866465167);
+    p = fma(p, f, 0.24022650695910075);
+    p = fma(p, f, 0.6931471805599462);
     p = fma(p, f, 1.0);
-    return ldexp(p, (int)n + e);
+    return ldexp(p, (int)n);
   }
-  // (a sum with 2^52 has the whole number, rounded, in its low bits)
-  __device__ __forceinline__ unsigned long long mass(double x) const {
-    return (unsigned long long)__double_as_longlong(power(fmax(x, -200.0), S) + 4503599627370496.0) & 0xfffffffffffffull;
+  // The weight times 2^S as a whole number; 0 for NaN and -inf.  (A sum with 2^52 has the whole number, rounded, in its low bits.)  The largest logit must be
+  // finite here, or l is it.
+  __device__ __forceinline__ unsigned long long mass(float l) const {
+    const double t = l == INFINITY ? (double)S : fma((double)l - (double)lmax, c, (double)S);
+    return (unsigned long long)__double_as_longlong(power(fmax(t, -64.0)) + 4503599627370496.0) & 0xfffffffffffffull;
   }
+  __device__ __forceinline__ unsigned long long mass_finite(float l) const {
+    return (unsigned long long)__double_as_longlong(power(fmax(fma((double)l - (double)lmax, c, (double)S), -64.0)) + 4503599627370496.0) & 0xfffffffffffffull;
+  }
+  __device__ __forceinline__ bool heavy(double x, float min_p) const { return power(fmax(x, -1100.0)) >= (double)min_p; }
 };
 
 struct SrFound { float value; int index; SrSum through; };   // the token at which the sum passes the target, and the sum up to and with it
@@ -113,7 +118,7 @@ __device__ inline SrFound sr_find(const float* row, int V, int index_bits, const
       if (!R.counts(l, x)) continue;
       const int bin = on_logit ? (int)(digit - (o >> shift & digit)) : (int)((uint32_t)i >> shift & digit);
       atomicAdd(&sh.count[bin], 1u);
-      atomicAdd(&sh.mass[bin], R.mass(x));
+      atomicAdd(&sh.mass[bin], R.mass(l));
     }
     __syncthreads();
     // two bins a thread: the running sum, and the one that passes
@@ -140,7 +145,7 @@ __device__ inline SrFound sr_find(const float* row, int V, int index_bits, const
     else { at |= bin << shift; at_mask |= digit << shift; }
   }
   const float value = sr_value(hi);
-  return {value, (int)at, before + SrSum{R.mass(R.log2w(value)), 1u}};
+  return {value, (int)at, before + SrSum{R.mass(value), 1u}};
 }
 
 // ---- a row in three looks --------------------------------------------------------------------------------------------------
@@ -163,25 +168,32 @@ struct SrFast {
 };
 union SrLds { SrShared slow; SrFast fast; };
 
-// f(logit, index) of every logit of the row, a thread's four at a time, SR_U pieces in flight.
+// f(logit, index) of every logit of the row, a thread's four at a time, SR_U pieces looked at while the next SR_U are on their way.
 template <typename F> __device__ __forceinline__ void sr_each(const float* row, int V, F f) {
-  const int pieces = V / 4, tid = threadIdx.x;
-  int i = tid;
-  for (; i + (SR_U - 1) * SR_THREADS < pieces; i += SR_U * SR_THREADS) {
-    SrFour x[SR_U];
+  const int pieces = V / 4, tid = threadIdx.x, mine = pieces > tid ? (pieces - tid + SR_THREADS - 1) / SR_THREADS : 0;
+  SrFour a[SR_U], b[SR_U];
+  auto fetch = [&](SrFour (&x)[SR_U], int i) __attribute__((always_inline)) {
 #pragma unroll
-    for (int u = 0; u < SR_U; ++u) x[u] = *reinterpret_cast<const SrFour*>(row + 4 * (i + u * SR_THREADS));
+    for (int u = 0; u < SR_U; ++u) x[u] = *reinterpret_cast<const SrFour*>(row + 4 * (tid + SR_THREADS * min(i + u, mine - 1)));     // (past the end: a piece there is)
+  };
+  auto look = [&](const SrFour (&x)[SR_U], int i) __attribute__((always_inline)) {
 #pragma unroll
     for (int u = 0; u < SR_U; ++u)
+      if (i + u < mine)
 #pragma unroll
-      for (int e = 0; e < 4; ++e) f(x[u].v[e], 4 * (i + u * SR_THREADS) + e);
+        for (int e = 0; e < 4; ++e) f(x[u].v[e], 4 * (tid + SR_THREADS * (i + u)) + e);
+  };
+  const float last = tid < V - 4 * pieces ? row[4 * pieces + tid] : 0.f;
+  if (mine > 0) {
+    fetch(a, 0);
+    for (int i = 0; i < mine; i += 2 * SR_U) {
+      if (i + SR_U < mine) fetch(b, i + SR_U);
+      look(a, i);
+      if (i + 2 * SR_U < mine) fetch(a, i + 2 * SR_U);
+      if (i + SR_U < mine) look(b, i + SR_U);
+    }
   }
-  for (; i < pieces; i += SR_THREADS) {
-    const SrFour x = *reinterpret_cast<const SrFour*>(row + 4 * i);
-#pragma unroll
-    for (int e = 0; e < 4; ++e) f(x.v[e], 4 * i + e);
-  }
-  if (tid < V - 4 * pieces) f(row[4 * pieces + tid], 4 * pieces + tid);
+  if (tid < V - 4 * pieces) f(last, 4 * pieces + tid);
 }
 __device__ __forceinline__ unsigned long long sr_key(float l, int i) { return (unsigned long long)sr_order(l) << 32 | (uint32_t)~i; }
 
@@ -249,6 +261,11 @@ __device__ __forceinline__ unsigned long long sr_pass(float u, unsigned long lon
 struct SrRules { float u, top_p, min_p; int top_k; bool greedy; };
 struct SrOut { int token; float value; unsigned long long kept_mass; int kept; };
 
+// Equal parts of [lmax - range, lmax], a logit's part is (lmax - l) times this; what weighs less than 2^-66 is in the last one.
+__device__ __forceinline__ float sr_parts(const SrRow& R, float lmin) {
+  const float range = fminf(R.lmax - lmin, (float)(66.0 / R.c));
+  return range > 1e-30f && range < INFINITY ? (SR_BINS - 1) / range : 0.f;
+}
 struct SrFirst { float value; int index; };                // a thread's own largest logit
 // False: the list did not fit.
 __device__ inline bool sr_fast(const float* row, int V, const SrRow& R, const SrRules& Q, SrFirst first, float lmin, SrFast& sh, SrOut& out) {
@@ -256,6 +273,7 @@ __device__ inline bool sr_fast(const float* row, int V, const SrRow& R, const Sr
   const bool by_prefix = Q.top_k > 0 && Q.top_k <= SR_TOPK, whole = V <= SR_LIST;
   const bool cut_p = !Q.greedy && Q.top_p < 1.f, cut_m = !Q.greedy && Q.min_p > 0.f;
   if (Q.top_k > SR_TOPK && Q.top_k < V && !whole) return false;
+  if (!(whole || by_prefix) && !(R.lmax < INFINITY)) return false;
   if (tid == 0) { sh.found = 0; sh.first_c = 0; sh.base_c = sh.base_d = 0ull; sh.c1 = 0; sh.c2 = SR_BINS; sh.d1 = 0; sh.d2 = SR_BINS; }
   __syncthreads();
   if (whole || by_prefix) {
@@ -286,18 +304,20 @@ __device__ inline bool sr_fast(const float* row, int V, const SrRow& R, const Sr
     });
   } else {
     // masses over equal parts of [lmax - range, lmax]; what weighs less than 2^-66 is in the last part
-    const float span = R.lmax - lmin, most = (float)(66.0 / R.c), range = fminf(span, most);
-    const float inv = range > 0.f && range < INFINITY ? (SR_BINS - 1) / range : 0.f;
-    auto part = [&](float l) __attribute__((always_inline)) { return l == R.lmax ? 0 : (int)fminf((R.lmax - l) * inv, (float)(SR_BINS - 1)); };
+    const float inv = sr_parts(R, lmin);
+    auto part = [&](float l) __attribute__((always_inline)) { return (int)fminf((R.lmax - l) * inv, (float)(SR_BINS - 1)); };
     for (int i = tid; i < SR_BINS; i += SR_THREADS) sh.hist[i] = 0ull;
     __syncthreads();
     unsigned mine = 0;
-    sr_each(row, V, [&](float l, int) {
-      const double x = R.log2w(l);
-      if (!R.counts(l, x)) return;
-      ++mine;
-      atomicAdd(&sh.hist[part(l)], R.mass(x));
-    });
+    auto add = [&](float l) __attribute__((always_inline)) {
+      const unsigned long long w = R.mass_finite(l);
+      if (w != 0) atomicAdd(&sh.hist[part(l)], w);         // (what weighs nothing would crowd the last part)
+    };
+    if (cut_p || cut_m) {
+      sr_each(row, V, [&](float l, int) { add(l); });
+    } else {
+      sr_each(row, V, [&](float l, int) { add(l); mine += R.counts(l, R.log2w(l)); });
+    }
     __syncthreads();
     const unsigned long long h0 = sh.hist[2 * tid], h1 = sh.hist[2 * tid + 1];
     unsigned long long total;
@@ -345,7 +365,7 @@ __device__ inline bool sr_fast(const float* row, int V, const SrRow& R, const Sr
       if (!(l > -INFINITY)) return;
       const int b = part(l);
       ahead += b < c1;
-      if (!((b >= c1 && b <= c2) || (b >= d1 && b <= d2))) return;
+      if ((unsigned)(b - c1) > (unsigned)(c2 - c1) && (unsigned)(b - d1) > (unsigned)(d2 - d1)) return;
       const int to = atomicAdd(&sh.found, 1);
       if (to < SR_LIST) sh.list[to] = sr_key(l, i);
     });
@@ -362,8 +382,7 @@ __device__ inline bool sr_fast(const float* row, int V, const SrRow& R, const Sr
 
   // The list in order, four tokens a thread: running sums.  by parts: the draw's tokens come first, then (or among them) the cuts'; sums start at the parts' own.
   const bool lists_all = whole || by_prefix;
-  const float span = R.lmax - lmin, most = (float)(66.0 / R.c), range = fminf(span, most);
-  const float inv = range > 0.f && range < INFINITY ? (SR_BINS - 1) / range : 0.f;
+  const float inv = sr_parts(R, lmin);
   const int c1 = sh.c1, d2 = sh.d2;
   const bool apart = !lists_all && d2 + 1 < c1;            // the cuts' parts do not touch the draw's
   const int limit = Q.top_k > 0 ? Q.top_k : SR_LIST;
@@ -378,9 +397,9 @@ __device__ inline bool sr_fast(const float* row, int V, const SrRow& R, const Sr
     value[e] = sr_value((uint32_t)(key >> 32));
     const double x = R.log2w(value[e]);
     ok[e] = i < n && (!lists_all || i < limit) && R.counts(value[e], x);
-    w[e] = ok[e] ? R.mass(x) : 0ull;
-    heavy[e] = ok[e] && (!cut_m || R.power(fmax(x, -1100.0), 0) >= (double)Q.min_p);
-    const int b = lists_all ? 0 : value[e] == R.lmax ? 0 : (int)fminf((R.lmax - value[e]) * inv, (float)(SR_BINS - 1));
+    w[e] = ok[e] ? R.mass(value[e]) : 0ull;
+    heavy[e] = ok[e] && (!cut_m || R.heavy(x, Q.min_p));
+    const int b = lists_all ? 0 : (int)fminf((R.lmax - value[e]) * inv, (float)(SR_BINS - 1));
     c_part[e] = lists_all || b >= c1;
     sum += w[e];
     in_d += c_part[e] ? 0ull : w[e];
@@ -491,9 +510,9 @@ __global__ void __launch_bounds__(SR_THREADS) k_sample_row(SampleArgs P) {
       const float l = row[i];
       const double x = R.log2w(l);
       if (!R.counts(l, x)) continue;
-      const SrSum one = {R.mass(x), 1u};
+      const SrSum one = {R.mass(l), 1u};
       all = all + one;
-      if (R.power(fmax(x, -1100.0), 0) >= (double)Q.min_p) heavy = heavy + one;
+      if (R.heavy(x, Q.min_p)) heavy = heavy + one;
     }
     SrShared& sh = lds.slow;
     all = sr_block_sum(all, sh);

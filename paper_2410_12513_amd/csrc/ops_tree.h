@@ -5,6 +5,8 @@
 // fetched once for all nodes and all of its query heads.  The keys are cut into splits; a workgroup walks one in tiles, with running maximum and
 // sum, and where there are several splits a second kernel joins them.  Split 0 begins with the tree's own keys.
 #pragma once
+#include <type_traits>
+
 #include "mfma_tiles.h"
 
 namespace first {
@@ -90,7 +92,12 @@ __global__ void __launch_bounds__(QG * KH * 64, QG == 1 ? 1 : 2) k_tree_attn(Tre
   {
     const char* x = reinterpret_cast<const char*>(P.q) + orow * RB + gl * 16;
 #pragma unroll
-    for (int s = 0; s < KS; ++s) Q[s] = *reinterpret_cast<const u32x4_t*>(x + s * 32);
+    for (int s = 0; s < KS; ++s) {
+      Q[s] = *reinterpret_cast<const u32x4_t*>(x + s * 32);
+      if (P.scale < 0.f)                                   // (the sign goes to the queries: a maximum of scores is then one of exponents)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) Q[s][e] ^= sizeof(E) == 2 ? 0x80008000u : 0x80000000u;
+    }
   }
   // what this lane fetches of a tile's keys and values, and where that lies in a page
   const int lrow = lane / CPR;
@@ -111,8 +118,8 @@ __global__ void __launch_bounds__(QG * KH * 64, QG == 1 ? 1 : 2) k_tree_attn(Tre
 #pragma unroll
       for (int i = 0; i < NI; ++i) {
         const uint32_t j = t * TK + (wave * NI + i) * RPL + lrow, off = j < (uint32_t)q.n ? j * pitch : 0x7ffffe00u;   // (no such node: zeros)
-        pg_load_lds(at + i * 1024, off + ck[i], rk, 0u);
-        pg_load_lds(at + KB + i * 1024, off + cv[i], rv, 0u);
+        pg_load_lds_any(at + i * 1024, off + ck[i], rk, 0u);
+        pg_load_lds_any(at + KB + i * 1024, off + cv[i], rv, 0u);
       }
       return;
     }
@@ -122,8 +129,8 @@ __global__ void __launch_bounds__(QG * KH * 64, QG == 1 ? 1 : 2) k_tree_attn(Tre
       const int r = (wave * NI + i) * RPL, pg = (k0 + r) / TREE_PAGE, id = pg < n_pg ? __builtin_amdgcn_readfirstlane(pages[pg]) : -1;
       const i32x4_t rs = pg_rsrc(reinterpret_cast<const char*>(P.pool) + (size_t)max(id, 0) * page_bytes, id >= 0 ? (uint32_t)page_bytes : 0u);
       const uint32_t off = k_lo + k0 + r + lrow < k_hi ? (uint32_t)(g * TREE_PAGE + r % TREE_PAGE + lrow) * RB : 0x7ff00000u;   // (past the end: zeros)
-      pg_load_lds(at + i * 1024, off + ck[i], rs, 0u);
-      pg_load_lds(at + KB + i * 1024, off + (uint32_t)P.Hkv * TREE_PAGE * RB + cv[i], rs, 0u);
+      pg_load_lds_any(at + i * 1024, off + ck[i], rs, 0u);
+      pg_load_lds_any(at + KB + i * 1024, off + (uint32_t)P.Hkv * TREE_PAGE * RB + cv[i], rs, 0u);
     }
   };
 
@@ -133,7 +140,7 @@ __global__ void __launch_bounds__(QG * KH * 64, QG == 1 ? 1 : 2) k_tree_attn(Tre
 #pragma unroll
     for (int r = 0; r < 16; ++r) O[t][r] = 0.f;
   float m = -INFINITY, l = 0.f;
-  const float sl = P.scale * LOG2E;
+  const float sl = fmaxf(fabsf(P.scale) * LOG2E, 1.17549435e-38f);       // (never 0: that of a masked score stays -inf)
   // bits of the 32 nodes from j0 on that this lane's row sees, moved so that bit 8 (r / 4) + r % 4 is that of register r
   auto seen = [&](int j0) __attribute__((always_inline)) {
     const int left = q.n - j0;
@@ -144,44 +151,45 @@ __global__ void __launch_bounds__(QG * KH * 64, QG == 1 ? 1 : 2) k_tree_attn(Tre
     }
     return w >> (4 * gl);
   };
-#pragma unroll
-  for (int t = 0; t < S - 1; ++t)
-    if (t < n_tiles) issue(t, t);
-  int slot = 0;
-  for (int t = 0; t < n_tiles; ++t) {
-    if (t + S - 2 < n_tiles) pg_wait<2 * NI * (S - 2)>(); else pg_wait<0>();
-    lds_barrier();
-    if (t + S - 1 < n_tiles) issue(t + S - 1, slot == 0 ? S - 1 : slot - 1);
-    const char* sk = tree_smem + slot * STG;
+  // One tile: n keys of it exist from the wave's first one on, k0 that key's number in the split or the tree.
+  auto tile = [&](auto tree, const char* sk, int k0, int n) __attribute__((always_inline)) {
     const char* sv = sk + KB;
-    slot = slot + 1 == S ? 0 : slot + 1;
-    const bool tree = t < n_tree;
-    const int k0 = tree ? t * TK + kh * NS * 32 : (t - n_tree) * TK + kh * NS * 32;      // this wave's first key
-    if (!live || k0 >= (tree ? q.n : k_hi - k_lo)) continue;
     floatx16_t W[NS];
 #pragma unroll
     for (int u = 0; u < NS; ++u)
 #pragma unroll
       for (int r = 0; r < 16; ++r) W[u][r] = 0.f;
+    {                                                      // (fragments requested in two halves ahead of the products: one by one, each product waited for its own)
+      constexpr int H = sizeof(E) == 4 ? 2 : KS / 2;
+      u32x4_t kf[2][H][NS];
+      auto fetch = [&](int h) __attribute__((always_inline)) {
 #pragma unroll
-    for (int s = 0; s < KS; ++s)
+        for (int s = 0; s < H; ++s)
 #pragma unroll
-      for (int u = 0; u < NS; ++u) {
-        const int row = (kh * NS + u) * 32 + col;
-        tree_mma(E{}, W[u], *reinterpret_cast<const u32x4_t*>(sk + row * RB + tree_kslot<RB>(row, 2 * s + gl) * 16), Q[s]);
+          for (int u = 0; u < NS; ++u) {
+            const int row = (kh * NS + u) * 32 + col;
+            kf[h & 1][s][u] = *reinterpret_cast<const u32x4_t*>(sk + row * RB + tree_kslot<RB>(row, 2 * (h * H + s) + gl) * 16);
+          }
+      };
+      fetch(0);
+#pragma unroll
+      for (int h = 0; h < KS / H; ++h) {
+        if (h + 1 < KS / H) fetch(h + 1);
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int s = 0; s < H; ++s)
+#pragma unroll
+          for (int u = 0; u < NS; ++u) tree_mma(E{}, W[u], kf[h & 1][s][u], Q[h * H + s]);
       }
-#pragma unroll
-    for (int u = 0; u < NS; ++u)
-#pragma unroll
-      for (int r = 0; r < 16; ++r) W[u][r] *= sl;
-    if (tree || k0 + NS * 32 > k_hi - k_lo || holes) {
+    }
+    if (tree || n < NS * 32 || holes) {
 #pragma unroll
       for (int u = 0; u < NS; ++u) {
         uint32_t w;
         if (tree) {
           w = seen(k0 + 32 * u);
         } else {
-          const int at = k0 + 32 * u, left = k_hi - k_lo - at, pg = at / TREE_PAGE;
+          const int left = n - 32 * u, pg = (k0 + 32 * u) / TREE_PAGE;
           w = left >= 32 ? ~0u : left <= 0 ? 0u : (1u << left) - 1u;
           if (holes) w &= (pg < n_pg && pages[pg] >= 0 ? 0xffffu : 0u) | (pg + 1 < n_pg && pages[pg + 1] >= 0 ? 0xffff0000u : 0u);
           w >>= 4 * gl;
@@ -197,7 +205,8 @@ __global__ void __launch_bounds__(QG * KH * 64, QG == 1 ? 1 : 2) k_tree_attn(Tre
       for (int r = 0; r < 16; ++r) mt = fmaxf(mt, W[u][r]);
     float ma, mb;
     both_halves(mt, ma, mb);
-    const float mn = fmaxf(m, fmaxf(ma, mb)), mu = mn == -INFINITY ? 0.f : mn;           // (nothing seen yet: weights of 0)
+    // (the maximum as it enters the exponent, rounded once after its product: a weight is 2^(s sl - m) with one rounding of that difference)
+    const float mn = fmaxf(m, fmaxf(ma, mb) * sl), mu = mn == -INFINITY ? 0.f : mn;      // (nothing seen yet: weights of 0)
     if (__any(mn > m)) {
       const float corr = __builtin_amdgcn_exp2f(m - mu);
       l *= corr;
@@ -211,15 +220,13 @@ __global__ void __launch_bounds__(QG * KH * 64, QG == 1 ? 1 : 2) k_tree_attn(Tre
 #pragma unroll
     for (int u = 0; u < NS; ++u)
 #pragma unroll
-      for (int r = 0; r < 16; ++r) { W[u][r] = __builtin_amdgcn_exp2f(W[u][r] - mu); ls[r & 3] += W[u][r]; }
+      for (int r = 0; r < 16; ++r) { W[u][r] = __builtin_amdgcn_exp2f(fmaf(W[u][r], sl, -mu)); ls[r & 3] += W[u][r]; }
     l += (ls[0] + ls[1]) + (ls[2] + ls[3]);
     if constexpr (sizeof(E) == 2) {
       // k-step s2 of a block: keys 16 s2 + 4 gl + 0..3 and 8 more, the rows of registers 8 s2 .. 8 s2 + 7
 #pragma unroll
       for (int s2 = 0; s2 < 2 * NS; ++s2) {
         union { uint32_t w[4]; u32x4_t x; } ph, pl;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) split_pair(W[s2 / 2][8 * (s2 & 1) + 2 * e], W[s2 / 2][8 * (s2 & 1) + 2 * e + 1], ph.w[e], pl.w[e]);
         const int row = kh * NS * 32 + 16 * s2 + 4 * gl + ((lane & 15) >> 2);
         u32x4_t vf[DT];
 #pragma unroll
@@ -231,6 +238,8 @@ __global__ void __launch_bounds__(QG * KH * 64, QG == 1 ? 1 : 2) k_tree_attn(Tre
             f.s[e] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((tree_lds4_t)(sv + (row + 8 * e) * RB + tree_vslot<E, RB>(row + 8 * e, chunk) * 16 + (lane & 1) * 8));
           vf[d] = f.x;
         }
+#pragma unroll
+        for (int e = 0; e < 4; ++e) split_pair(W[s2 / 2][8 * (s2 & 1) + 2 * e], W[s2 / 2][8 * (s2 & 1) + 2 * e + 1], ph.w[e], pl.w[e]);
 #pragma unroll
         for (int d = 0; d < DT; ++d) tree_mma(E{}, O[d], vf[d], pl.x);
 #pragma unroll
@@ -248,40 +257,64 @@ __global__ void __launch_bounds__(QG * KH * 64, QG == 1 ? 1 : 2) k_tree_attn(Tre
                                                         W[u][r], O[d], 0, 0, 0);
         }
     }
-    if (tree && (t + 1) * TK + kh * NS * 32 >= q.n) {       // the wave's last keys of the tree
-      // The products above take nodes that a row does not see times 0: an infinity or NaN there must not reach the row.  Where any is about (rare),
-      // the wave's share of the tree again, a key at a time and only the seen ones.
-      bool odd = false;
+  };
+  // The products take nodes that a row does not see times 0: an infinity or NaN there must not reach the row.  Where any is about (rare), the wave's share of
+  // the tree again, a key at a time and only the seen ones.
+  auto again = [&]() __attribute__((always_inline)) {
+    bool odd = false;
+#pragma unroll
+    for (int d = 0; d < DT; ++d)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) odd |= !(fabsf(O[d][r]) < INFINITY);
+    if (!__any(odd)) return;
+    m = -INFINITY; l = 0.f;
+#pragma unroll
+    for (int d = 0; d < DT; ++d)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) O[d][r] = 0.f;
+    const E* qr = reinterpret_cast<const E*>(P.q) + orow * HD;
+    const float sc = P.scale < 0.f ? -sl : sl;
+    for (int j = 0; j < q.n; ++j) {
+      if (j / (NS * 32) % KH != kh) continue;
+      if (P.mask != nullptr ? !(P.mask[(size_t)(q.o0 + node) * P.words + j / 64] >> (j % 64) & 1) : j > node) continue;
+      const size_t at = ((size_t)(q.o0 + j) * P.Hkv + g) * HD;
+      const E *kr = reinterpret_cast<const E*>(P.k) + at, *vr = reinterpret_cast<const E*>(P.v) + at;
+      float s = 0.f;
+      for (int d = 0; d < HD; ++d) s = fmaf(to_f32(qr[d]), to_f32(kr[d]), s);
+      s *= sc;
+      const float top = fmaxf(m, s), use = top == -INFINITY ? 0.f : top, c = __builtin_amdgcn_exp2f(m - use), w = __builtin_amdgcn_exp2f(s - use);
+      m = top;
+      l = l * c + (gl == 0 ? w : 0.f);                     // (both halves of the wave hold the row, and add their sums at the end)
 #pragma unroll
       for (int d = 0; d < DT; ++d)
 #pragma unroll
-        for (int r = 0; r < 16; ++r) odd |= !(fabsf(O[d][r]) < INFINITY);
-      if (__any(odd)) {
-        m = -INFINITY; l = 0.f;
-#pragma unroll
-        for (int d = 0; d < DT; ++d)
-#pragma unroll
-          for (int r = 0; r < 16; ++r) O[d][r] = 0.f;
-        const E* qr = reinterpret_cast<const E*>(P.q) + orow * HD;
-        for (int j = 0; j < q.n; ++j) {
-          if (j / (NS * 32) % KH != kh) continue;
-          const bool mine = P.mask != nullptr ? P.mask[(size_t)(q.o0 + node) * P.words + j / 64] >> (j % 64) & 1 : j <= node;
-          if (!mine) continue;
-          const size_t at = ((size_t)(q.o0 + j) * P.Hkv + g) * HD;
-          const E *kr = reinterpret_cast<const E*>(P.k) + at, *vr = reinterpret_cast<const E*>(P.v) + at;
-          float s = 0.f;
-          for (int d = 0; d < HD; ++d) s = fmaf(to_f32(qr[d]), to_f32(kr[d]), s);
-          s *= sl;
-          const float top = fmaxf(m, s), use = top == -INFINITY ? 0.f : top, c = __builtin_amdgcn_exp2f(m - use), w = __builtin_amdgcn_exp2f(s - use);
-          m = top;
-          l = l * c + (gl == 0 ? w : 0.f);                 // (both halves of the wave hold the row, and add their sums at the end)
-#pragma unroll
-          for (int d = 0; d < DT; ++d)
-#pragma unroll
-            for (int r = 0; r < 16; ++r) O[d][r] = fmaf(w, to_f32(vr[32 * d + 8 * (r >> 2) + 4 * gl + (r & 3)]), O[d][r] * c);
-        }
-      }
+        for (int r = 0; r < 16; ++r) O[d][r] = fmaf(w, to_f32(vr[32 * d + 8 * (r >> 2) + 4 * gl + (r & 3)]), O[d][r] * c);
     }
+  };
+
+#pragma unroll
+  for (int t = 0; t < S - 1; ++t)
+    if (t < n_tiles) issue(t, t);
+  int slot = 0;
+  auto arrived = [&](int t) __attribute__((always_inline)) {          // tile t is there; the tile S - 1 ahead is requested
+    if (t + S - 2 < n_tiles) pg_wait<2 * NI * (S - 2)>(); else pg_wait<0>();
+    lds_barrier();
+    if (t + S - 1 < n_tiles) issue(t + S - 1, slot == 0 ? S - 1 : slot - 1);
+    const char* at = tree_smem + slot * STG;
+    slot = slot + 1 == S ? 0 : slot + 1;
+    return at;
+  };
+  int t = 0;
+  for (; t < n_tree; ++t) {
+    const char* at = arrived(t);
+    const int k0 = t * TK + kh * NS * 32;
+    if (live && k0 < q.n) tile(std::true_type{}, at, k0, q.n - k0);
+  }
+  if (live && n_tree > 0) again();
+  for (; t < n_tiles; ++t) {
+    const char* at = arrived(t);
+    const int k0 = (t - n_tree) * TK + kh * NS * 32, n = k_hi - k_lo - k0;
+    if (live && n > 0) tile(std::false_type{}, at, k0, n);
   }
   float la, lb;
   both_halves(l, la, lb);
