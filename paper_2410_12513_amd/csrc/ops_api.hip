@@ -36,15 +36,16 @@ int64_t up(int64_t x, int64_t to) { return (x + to - 1) / to * to; }
 
 constexpr int CUS = 256;                  // compute units of the MI355X
 
-// Launches; a kernel that may use more than 64 KB of LDS is told so first, once a device.
-template <auto kernel, typename Args> hipError_t launch(hipStream_t st, dim3 grid, int threads, size_t lds, const Args& P) {
-  if (lds > 64 * 1024) {
+// Launches; a kernel that may use more than 64 KB of LDS is told so first, once a device: `most` bytes of dynamic LDS in any call (0: lds, always the same).
+template <auto kernel, typename Args> hipError_t launch(hipStream_t st, dim3 grid, int threads, size_t lds, const Args& P, size_t most = 0) {
+  if (most == 0) most = lds;
+  if (most > 32 * 1024) {
     static std::atomic<uint64_t> told{0};
     int dev = 0;
     hipError_t e = hipGetDevice(&dev);
     if (e != hipSuccess) return e;
     if (dev >= 64 || !(told.load(std::memory_order_relaxed) >> dev & 1)) {
-      e = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
+      e = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (int)most);
       if (e != hipSuccess) return e;
       if (dev < 64) told.fetch_or(1ull << dev, std::memory_order_relaxed);
     }
@@ -87,7 +88,7 @@ template <typename E> hipError_t launch_lora(hipStream_t st, LoraArgs& P, const 
     const int grid = helpers + (P.n + 63) / 64 * P.ks;
     e = P.m <= 16 ? launch<&k_lora_stream<E, 16, 6>>(st, grid, WG, LORA_A_BYTES + 4 * 6 * 2048, P) : launch<&k_lora_stream<E, 32, 6>>(st, grid, WG, LORA_A_BYTES + 4 * 6 * 2048, P);
   } else {
-    e = launch<&k_lora_shrink<E>>(st, helpers, LORA_SHRINK_WAVES * 64, (size_t)LORA_SHRINK_WAVES * 16 * P.rp * 4, P);
+    e = launch<&k_lora_shrink<E>>(st, helpers, LORA_SHRINK_WAVES * 64, (size_t)LORA_SHRINK_WAVES * 16 * P.rp * 4, P, (size_t)LORA_SHRINK_WAVES * 16 * LORA_RMAX * 4);
     if (e != hipSuccess) return e;
     P.gm = (P.m + plan.tile - 1) / plan.tile;
     P.gn = (P.n + plan.tile - 1) / plan.tile;
@@ -279,8 +280,7 @@ int first_sample(void* hip_stream, const float* logits, int64_t pitch, int32_t r
   int bits = 0;
   while (bits < 31 && (int64_t)1 << bits < vocab) ++bits;
   SampleArgs P = {logits, pitch, vocab, bits, std::min(50, 62 - bits), uniforms, temperature, top_k, top_p, min_p, token_out, logprob_out, kept_out};
-  hipLaunchKernelGGL(k_sample_row, dim3(rows), dim3(SR_THREADS), 0, stream_of(hip_stream), P);
-  return launched("first_sample");
+  return launched("first_sample", launch<&k_sample_row>(stream_of(hip_stream), dim3(rows), SR_THREADS, 0, P));
 }
 
 }  // extern "C"

@@ -152,15 +152,14 @@ __device__ inline SrFound sr_find(const float* row, int V, int index_bits, const
 // What can be drawn and where the cuts lie is decided among a few tokens, a list in LDS that is put in order; what is not on it only matters by its sum.
 //   with top_k (up to SR_TOPK), or few tokens: the k-th largest of the threads' (of groups' of 16 threads) own maxima is a bound that at least k tokens reach; the
 //     list is what reaches it, and no other weight is formed;
-//   else: a histogram of the masses over 2048 equal parts of the range of logits that weigh anything says in which part each cut lies, and in which few the draw
+//   else: a histogram of the masses over 4096 equal parts of the range of logits that weigh anything says in which part each cut lies, and in which few the draw
 //     can lie; the list is those parts' tokens.
 // A list that does not fit (masses of equal logits, logits that crowd one part) is left for the digit by digit search over the whole row.
-constexpr int SR_LIST = 4096, SR_TOPK = 960, SR_U = 4;
+constexpr int SR_LIST = 4096, SR_TOPK = 960, SR_U = 4, SR_PARTS = 4096;
 struct __align__(4) SrFour { float v[4]; };               // (a row starts on 4 bytes)
 
 struct SrFast {
-  unsigned long long list[SR_LIST];
-  unsigned long long hist[SR_BINS];
+  union { unsigned long long list[SR_LIST], hist[SR_PARTS]; };            // (the histogram is through before the list begins)
   unsigned long long wave[SR_WAVES], base_c, base_d, total, kept_mass;
   int found, first_c, cut_p, cut_m, kept, pick, c1, c2, d1, d2;
   unsigned count[SR_WAVES];
@@ -216,14 +215,16 @@ __device__ inline void sr_sort(unsigned long long* list, int n) {
   while (size < n) size *= 2;
   for (int i = n + tid; i < size; i += SR_THREADS) list[i] = 0ull;
   __syncthreads();
-  for (int k = 2; k <= size; k *= 2)
-    for (int j = k / 2; j > 0; j /= 2) {
+  for (int k = 1; 1 << k <= size; ++k)
+    for (int j = k - 1; j >= 0; --j) {
       for (int t = tid; t < size / 2; t += SR_THREADS) {
-        const int i = 2 * j * (t / j) + t % j, o = i + j;
+        const int i = (t >> j << (j + 1)) + (t & ((1 << j) - 1)), o = i + (1 << j);
         const unsigned long long a = list[i], b = list[o];
-        if ((a < b) == ((i & k) == 0)) { list[i] = b; list[o] = a; }
+        if ((a < b) == ((i >> k & 1) == 0)) { list[i] = b; list[o] = a; }
       }
-      __syncthreads();
+      // (pairs up to 64 apart: a wave's own 128 keys)
+      if (j >= 7 || j == 0) __syncthreads();
+      else { __builtin_amdgcn_fence(__ATOMIC_SEQ_CST, "wavefront"); __builtin_amdgcn_wave_barrier(); }
     }
 }
 // Exclusive running sum over the threads, and the sum of all.
@@ -264,7 +265,7 @@ struct SrOut { int token; float value; unsigned long long kept_mass; int kept; }
 // Equal parts of [lmax - range, lmax], a logit's part is (lmax - l) times this; what weighs less than 2^-66 is in the last one.
 __device__ __forceinline__ float sr_parts(const SrRow& R, float lmin) {
   const float range = fminf(R.lmax - lmin, (float)(66.0 / R.c));
-  return range > 1e-30f && range < INFINITY ? (SR_BINS - 1) / range : 0.f;
+  return range > 1e-30f && range < INFINITY ? (SR_PARTS - 1) / range : 0.f;
 }
 struct SrFirst { float value; int index; };                // a thread's own largest logit
 // False: the list did not fit.
@@ -274,7 +275,7 @@ __device__ inline bool sr_fast(const float* row, int V, const SrRow& R, const Sr
   const bool cut_p = !Q.greedy && Q.top_p < 1.f, cut_m = !Q.greedy && Q.min_p > 0.f;
   if (Q.top_k > SR_TOPK && Q.top_k < V && !whole) return false;
   if (!(whole || by_prefix) && !(R.lmax < INFINITY)) return false;
-  if (tid == 0) { sh.found = 0; sh.first_c = 0; sh.base_c = sh.base_d = 0ull; sh.c1 = 0; sh.c2 = SR_BINS; sh.d1 = 0; sh.d2 = SR_BINS; }
+  if (tid == 0) { sh.found = 0; sh.first_c = 0; sh.base_c = sh.base_d = 0ull; sh.c1 = 0; sh.c2 = SR_PARTS; sh.d1 = 0; sh.d2 = SR_PARTS; }
   __syncthreads();
   if (whole || by_prefix) {
     unsigned long long bound = 0ull;
@@ -305,38 +306,38 @@ __device__ inline bool sr_fast(const float* row, int V, const SrRow& R, const Sr
   } else {
     // masses over equal parts of [lmax - range, lmax]; what weighs less than 2^-66 is in the last part
     const float inv = sr_parts(R, lmin);
-    auto part = [&](float l) __attribute__((always_inline)) { return (int)fminf((R.lmax - l) * inv, (float)(SR_BINS - 1)); };
-    for (int i = tid; i < SR_BINS; i += SR_THREADS) sh.hist[i] = 0ull;
+    auto part = [&](float l) __attribute__((always_inline)) { return (int)fminf((R.lmax - l) * inv, (float)(SR_PARTS - 1)); };
+    for (int i = tid; i < SR_PARTS; i += SR_THREADS) sh.hist[i] = 0ull;
     __syncthreads();
     unsigned mine = 0;
-    auto add = [&](float l) __attribute__((always_inline)) {
+    auto add = [&](float l, int b) __attribute__((always_inline)) {
       const unsigned long long w = R.mass_finite(l);
-      if (w != 0) atomicAdd(&sh.hist[part(l)], w);         // (what weighs nothing would crowd the last part)
+      if (w != 0) atomicAdd(&sh.hist[b], w);               // (what weighs nothing would crowd the last part)
     };
-    if (cut_p || cut_m) {
-      sr_each(row, V, [&](float l, int) { add(l); });
-    } else {
-      sr_each(row, V, [&](float l, int) { add(l); mine += R.counts(l, R.log2w(l)); });
-    }
+    sr_each(row, V, [&](float l, int) { add(l, part(l)); });
+    if (!cut_p && !cut_m) sr_each(row, V, [&](float l, int) { mine += R.counts(l, R.log2w(l)); });
     __syncthreads();
-    const unsigned long long h0 = sh.hist[2 * tid], h1 = sh.hist[2 * tid + 1];
-    unsigned long long total;
-    const unsigned long long before = sr_scan(h0 + h1, sh.wave, total);
+    unsigned long long h[4], total;                        // four parts a thread: the sums through them
+#pragma unroll
+    for (int e = 0; e < 4; ++e) h[e] = sh.hist[4 * tid + e] + (e > 0 ? h[e - 1] : 0ull);
+    const unsigned long long before = sr_scan(h[3], sh.wave, total);
+    auto sum_before = [&](int e) __attribute__((always_inline)) { return before + (e > 0 ? h[e - 1] : 0ull); };
     if (cut_m) {                                           // the parts in which w = min_p can lie
       const double l = (double)R.lmax + log2((double)Q.min_p) / R.c, off = 1e-6 * (fabs(l) + fabs((double)R.lmax));
       const int a = part((float)(l + off)), b = part((float)(l - off));
       if (tid == 0) { sh.c1 = min(a, b); sh.c2 = max(a, b); }
     }
-    // the first part at which the sum reaches x: f(part, sum before it, sum through it)
+    // the first part at which the sum reaches x: f(part, sum before it)
     auto at = [&](unsigned long long x, auto f) __attribute__((always_inline)) {
-      if (before < x && x <= before + h0) f(2 * tid, before, before + h0);
-      if (before + h0 < x && x <= before + h0 + h1) f(2 * tid + 1, before + h0, before + h0 + h1);
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        if (sum_before(e) < x && x <= before + h[e]) f(4 * tid + e, sum_before(e));
     };
     __syncthreads();
     if (cut_p) {
       const int c1 = sh.c1, c2 = sh.c2;
       __syncthreads();
-      at(sr_reach(Q.top_p, total), [&](int i, unsigned long long, unsigned long long) {
+      at(sr_reach(Q.top_p, total), [&](int i, unsigned long long) {
         if (!cut_m || i < c1) { sh.c1 = i; sh.c2 = i; }
         else if (i <= c2) sh.c2 = c2;
       });
@@ -346,18 +347,19 @@ __device__ inline bool sr_fast(const float* row, int V, const SrRow& R, const Sr
     // sums before c1 and through c2: what is kept lies between
     if (cut) {
       const int c1 = sh.c1, c2 = sh.c2;
-      if (2 * tid == c1) sh.base_c = before;
-      if (2 * tid + 1 == c1) sh.base_c = before + h0;
-      if (2 * tid == c2) sh.total = before + h0;
-      if (2 * tid + 1 == c2) sh.total = before + h0 + h1;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        if (4 * tid + e == c1) sh.base_c = sum_before(e);
+        if (4 * tid + e == c2) sh.total = before + h[e];
+      }
     } else if (tid == 0) {
       sh.base_c = sh.total = total;
-      sh.c1 = sh.c2 = SR_BINS;
+      sh.c1 = sh.c2 = SR_PARTS;
     }
     __syncthreads();
     const unsigned long long least = sh.base_c, largest = sh.total;
-    at(least > 0 ? sr_pass(Q.u, least) + 1 : 1ull, [&](int i, unsigned long long b, unsigned long long) { sh.d1 = i; sh.base_d = b; });
-    at(sr_pass(Q.u, largest) + 1, [&](int i, unsigned long long, unsigned long long) { sh.d2 = i; });
+    at(least > 0 ? sr_pass(Q.u, least) + 1 : 1ull, [&](int i, unsigned long long b) { sh.d1 = i; sh.base_d = b; });
+    at(sr_pass(Q.u, largest) + 1, [&](int i, unsigned long long) { sh.d2 = i; });
     __syncthreads();
     const int c1 = sh.c1, c2 = sh.c2, d1 = sh.d1, d2 = sh.d2;
     unsigned ahead = 0;                                    // tokens before c1
@@ -399,7 +401,7 @@ __device__ inline bool sr_fast(const float* row, int V, const SrRow& R, const Sr
     ok[e] = i < n && (!lists_all || i < limit) && R.counts(value[e], x);
     w[e] = ok[e] ? R.mass(value[e]) : 0ull;
     heavy[e] = ok[e] && (!cut_m || R.heavy(x, Q.min_p));
-    const int b = lists_all ? 0 : (int)fminf((R.lmax - value[e]) * inv, (float)(SR_BINS - 1));
+    const int b = lists_all ? 0 : (int)fminf((R.lmax - value[e]) * inv, (float)(SR_PARTS - 1));
     c_part[e] = lists_all || b >= c1;
     sum += w[e];
     in_d += c_part[e] ? 0ull : w[e];
