@@ -54,6 +54,17 @@ template <auto kernel, typename Args> hipError_t launch(hipStream_t st, dim3 gri
   return hipGetLastError();
 }
 
+// ---- rotary positions ------------------------------------------------------------------------------------------------------
+// Four rows a workgroup where that still leaves eight workgroups a compute unit, so that their sines are formed side by side.
+template <typename T> hipError_t launch_rope(hipStream_t st, const RopeArgs& P) {
+  constexpr int EPC = 16 / (int)sizeof(T);
+  const bool whole = (P.interleaved ? P.rot : P.rot / 2) % EPC == 0 && P.hd % EPC == 0 && P.x_pitch % EPC == 0 && P.y_pitch % EPC == 0 && aligned(P.x, 16) && aligned(P.y, 16);
+  if (!whole) return launch<&k_rope<T>>(st, dim3(P.rows), WG, 0, P);
+  if (P.rows >= 4 * 8 * CUS)
+    return P.interleaved ? launch<&k_rope_chunks<T, true, 4>>(st, dim3((P.rows + 3) / 4), WG, 0, P) : launch<&k_rope_chunks<T, false, 4>>(st, dim3((P.rows + 3) / 4), WG, 0, P);
+  return P.interleaved ? launch<&k_rope_chunks<T, true, 1>>(st, dim3(P.rows), WG, 0, P) : launch<&k_rope_chunks<T, false, 1>>(st, dim3(P.rows), WG, 0, P);
+}
+
 // ---- projections with an adapter per row -----------------------------------------------------------------------------------
 // stream: up to 32 rows, slices of K such that two workgroups a compute unit are busy, of four steps at least.  tile: the BM x BN with the least estimated time, rounds
 // of the chip times the tile's products over how well it feeds the matrix cores; slices of K where the tiles of one round leave half of the chip idle.
@@ -182,10 +193,8 @@ int first_op_rope(void* hip_stream, const first_rope_desc* d, const void* x, int
     }
     P.turns[i] = g / two_pi;
   }
-  const dim3 grid((unsigned)rows);
-  if (d->dtype == FIRST_DTYPE_BF16) hipLaunchKernelGGL(k_rope<bf16>, grid, dim3(WG), 0, stream_of(hip_stream), P);
-  else hipLaunchKernelGGL(k_rope<float>, grid, dim3(WG), 0, stream_of(hip_stream), P);
-  return launched("first_op_rope");
+  const hipStream_t st = stream_of(hip_stream);
+  return launched("first_op_rope", d->dtype == FIRST_DTYPE_BF16 ? launch_rope<bf16>(st, P) : launch_rope<float>(st, P));
 }
 
 int64_t first_op_gemm_nt_lora_workspace(int32_t dtype, int32_t m, int32_t n, int32_t k, int32_t r) {

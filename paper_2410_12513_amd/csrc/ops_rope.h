@@ -29,13 +29,80 @@ __device__ __forceinline__ float2 rope_cs(const RopeArgs& P, int pos, int i) {
   return make_float2(c * P.amplitude, s * P.amplitude * P.sign);
 }
 
-// grid (rows), a workgroup a row: the row's sines into LDS, then its heads.
+// Rows whose heads start on 16 bytes and whose pairs fill whole chunks of 16 bytes: a workgroup takes R rows, their sines into LDS (a pair of a row a
+// thread), then chunks of their heads: two of them, half a turned part apart (half), or one (interleaved) that hold whole pairs, or one that passes.
+// ROPE_U chunks of a thread on their way at a time.  Bound: HBM; a pass is one read and one write of the heads.
+constexpr int ROPE_U = 4;
+template <typename T, bool INTER, int R>
+__global__ void __launch_bounds__(WG) k_rope_chunks(RopeArgs P) {
+  constexpr int EPC = 16 / (int)sizeof(T), PAIRS = INTER ? EPC / 2 : EPC;
+  __shared__ __align__(16) float2 cs[R * ROPE_MAX_PAIRS];
+  const int half = P.rot / 2, turned = half / PAIRS, items = turned + (P.hd - P.rot) / EPC;      // of a head
+  const long long row0 = (long long)blockIdx.x * R;
+  const int rows = (int)min((long long)R, P.rows - row0);
+  for (int i = threadIdx.x; i < rows * half; i += WG) cs[i] = rope_cs(P, P.positions[row0 + i / half], i % half);
+  __syncthreads();
+  const int total = rows * P.heads * items;
+  const T* x0 = reinterpret_cast<const T*>(P.x) + row0 * P.x_pitch;
+  T* y0 = reinterpret_cast<T*>(P.y) + row0 * P.y_pitch;
+  for (int j0 = threadIdx.x; j0 < total; j0 += ROPE_U * WG) {
+    u32x4_t a[ROPE_U], b[ROPE_U];
+    int row[ROPE_U], at[ROPE_U], c[ROPE_U];
+#pragma unroll
+    for (int u = 0; u < ROPE_U; ++u) {
+      const int j = min(j0 + u * WG, total - 1), h = j / items;
+      c[u] = j - h * items;
+      row[u] = h / P.heads;
+      at[u] = (h - row[u] * P.heads) * P.hd + (c[u] < turned ? c[u] * EPC : P.rot + (c[u] - turned) * EPC);
+      const T* x = x0 + row[u] * P.x_pitch + at[u];
+      a[u] = *reinterpret_cast<const u32x4_t*>(x);
+      if (!INTER) b[u] = *reinterpret_cast<const u32x4_t*>(x + (c[u] < turned ? half : 0));
+    }
+#pragma unroll
+    for (int u = 0; u < ROPE_U; ++u) {
+      if (j0 + u * WG >= total) break;
+      T* y = y0 + row[u] * P.y_pitch + at[u];
+      if (c[u] >= turned) {
+        *reinterpret_cast<u32x4_t*>(y) = a[u];
+        continue;
+      }
+      const float2* w = cs + row[u] * half + c[u] * PAIRS;
+      float v[2 * PAIRS], o[2 * PAIRS];                    // half: the first elements, then the second; interleaved: as they stand
+      auto widen = [&](u32x4_t r, float* to) __attribute__((always_inline)) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          if constexpr (sizeof(T) == 2) { to[2 * e] = __uint_as_float(r[e] << 16); to[2 * e + 1] = __uint_as_float(r[e] & 0xffff0000u); }
+          else to[e] = __uint_as_float(r[e]);
+        }
+      };
+      widen(a[u], v);
+      if (!INTER) widen(b[u], v + EPC);
+#pragma unroll
+      for (int i = 0; i < PAIRS; ++i) {
+        const int ia = INTER ? 2 * i : i, ib = INTER ? 2 * i + 1 : i + PAIRS;
+        const float2 t = w[i];
+        o[ia] = v[ia] * t.x - v[ib] * t.y;
+        o[ib] = v[ia] * t.y + v[ib] * t.x;
+      }
+      auto narrow = [&](const float* from) __attribute__((always_inline)) {
+        u32x4_t r;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) r[e] = sizeof(T) == 2 ? pk_bf16(from[2 * e], from[2 * e + 1]) : __float_as_uint(from[e]);
+        return r;
+      };
+      *reinterpret_cast<u32x4_t*>(y) = narrow(o);
+      if (!INTER) *reinterpret_cast<u32x4_t*>(y + half) = narrow(o + EPC);
+    }
+  }
+}
+
+// Any other row: grid (rows), a workgroup a row, an element pair a thread.
 template <typename T>
 __global__ void __launch_bounds__(WG) k_rope(RopeArgs P) {
   __shared__ float2 cs[ROPE_MAX_PAIRS];
   const int half = P.rot / 2;
-  for (long long row = blockIdx.x; row < P.rows; row += gridDim.x) {
-    __syncthreads();
+  {
+    const long long row = blockIdx.x;
     for (int i = threadIdx.x; i < half; i += WG) cs[i] = rope_cs(P, P.positions[row], i);
     __syncthreads();
     const T* x = reinterpret_cast<const T*>(P.x) + row * P.x_pitch;
