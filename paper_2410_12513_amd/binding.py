@@ -379,14 +379,15 @@ def _raise(rc: int) -> None:
 
 
 def _device(t: torch.Tensor) -> int:
-    if not t.is_cuda:
+    dev = t.get_device()
+    if dev < 0:
         raise ValueError("expected device tensors")
-    return t.get_device()
+    return dev
 
 
 def _same(t: torch.Tensor, dtype: torch.dtype, shape, dev: int, name: str) -> int:
     """The address of a contiguous tensor of this type and shape on this device."""
-    if t.dtype is not dtype or t.shape != shape or not t.is_contiguous() or not t.is_cuda or t.get_device() != dev:
+    if t.dtype is not dtype or t.shape != shape or not t.is_contiguous() or t.get_device() != dev:        # (-1: not on a device)
         raise ValueError(f"{name}: expected a contiguous tensor of {dtype}, {list(shape)}, on device {dev}")
     return t.data_ptr()
 
@@ -399,13 +400,17 @@ def _code(t: torch.Tensor, name: str) -> int:
     raise ValueError(f"{name}: expected bfloat16 or float32")
 
 
+# the address of a device's current stream, without a Stream object around it where torch offers that
+_current = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda dev: torch.cuda.current_stream(dev).cuda_stream)
+
+
 def _launch(dev: int, stream, workspace: Optional[torch.Tensor], need, call) -> None:
     """call(stream, workspace address, bytes) with device `dev` current, on `stream` or its current stream; a workspace of need() bytes lives until
     that stream is through with it, unless the caller brings one."""
     if torch.cuda.current_device() != dev:
         with torch.cuda.device(dev):
             return _launch(dev, stream, workspace, need, call)
-    st = torch.cuda.current_stream(dev).cuda_stream if stream is None else stream.cuda_stream
+    st = _current(dev) if stream is None else stream.cuda_stream
     at = size = 0
     if workspace is not None:
         if workspace.get_device() != dev or not workspace.is_contiguous():
@@ -460,7 +465,7 @@ def op_rope(x: torch.Tensor, positions: torch.Tensor, y: torch.Tensor, rot_dim: 
     pitches = []
     for t, name in ((x, "x"), (y, "y")):
         st = t.stride()
-        if t.dtype is not x.dtype or t.shape != x.shape or not t.is_cuda or t.get_device() != dev or (rows and (st[2] != 1 or (heads > 1 and st[1] != hd))):
+        if t.dtype is not x.dtype or t.shape != x.shape or t.get_device() != dev or (rows and (st[2] != 1 or (heads > 1 and st[1] != hd))):
             raise ValueError(f"{name}: expected [rows, heads, head_dim] of one type on one device, the heads of a row one after the other")
         pitches.append(st[0] if rows > 1 else heads * hd)
     if layout not in ROPE_LAYOUTS or scaling not in ROPE_SCALINGS:

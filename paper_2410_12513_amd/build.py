@@ -28,7 +28,8 @@ FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-shared",
 # other way; "k_bgemv" covers k_bgemv and k_bgemv_g).  k_pgemm and k_attn_prompt load straight into LDS and wait by
 # counting the loads behind the one they need: a reload from scratch would be counted among them.
 SCRATCH_LIMITS = {"k_step": 0, "k_attn_tiles_b": 32, "k_attn_mfma_b": 0, "k_bgemv": 0, "k_gemm_nt_bf16_hl": 0,
-                  "k_pgemm": 0, "k_attn_prompt": 0, "k_small_step": 240, "k_batch_step": 0}
+                  "k_pgemm": 0, "k_attn_prompt": 0, "k_small_step": 240, "k_batch_step": 0, "k_tree_attn": 0, "k_lora_stream": 0,
+                  "k_lora_tile": 0}
 
 # Registers a lane (vector and accumulation ones together) of the two kernels whose workgroups wait for each other: a SIMD has 512, and two
 # waves of k_step and one of k_small_step have to fit on it together.  With more, a step of each on two streams could hold what the other

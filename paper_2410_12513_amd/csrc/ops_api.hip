@@ -71,19 +71,17 @@ template <typename T> hipError_t launch_rope(hipStream_t st, const RopeArgs& P) 
 struct LoraPlan { int tile, ks; };        // tile 0: stream
 LoraPlan lora_plan(int dtype, int m, int n, int k) {
   const int64_t steps = up((int64_t)k * size_of(dtype), 128) / 128;
-  if (m <= LORA_STREAM_ROWS) {
-    const int64_t groups = (n + 63) / 64;
-    const int64_t least = up(steps * 128 * (m <= 16 ? 16 : 32), LORA_A_BYTES) / LORA_A_BYTES;      // (a slice of A has to fit its place in LDS)
+  const int64_t groups = (n + 63) / 64, least = up(steps * 128 * (m <= 16 ? 16 : m <= 32 ? 32 : 64), LORA_A_BYTES) / LORA_A_BYTES;     // (a slice of A has to fit its place in LDS)
+  if (m <= 32 || (m <= LORA_STREAM_ROWS && least <= 4))
     return {0, (int)std::max(least, std::min((2 * CUS + groups / 2) / groups, steps / 4))};
-  }
   LoraPlan best = {64, 1};
-  double least = 1e300;
+  double fastest = 1e300;
   for (int t : {256, 128, 64}) {
     const int64_t tiles = (int64_t)((m + t - 1) / t) * ((n + t - 1) / t);
     const int64_t ks = m > 65535 ? 1 : std::max<int64_t>(1, std::min<int64_t>({CUS / tiles, steps / 8, 8}));
     const double feed = t == 256 ? 1.0 : t == 128 ? 0.75 : 0.45, rounds = (double)((tiles * ks + CUS - 1) / CUS);
     const double time = rounds * ((double)t * t / feed * ((steps + ks - 1) / ks) + 8 * t * t) + (ks > 1 ? 2e5 : 0);
-    if (time < least) { least = time; best = {t, (int)ks}; }
+    if (time < fastest) { fastest = time; best = {t, (int)ks}; }
   }
   return best;
 }
@@ -97,7 +95,8 @@ template <typename E> hipError_t launch_lora(hipStream_t st, LoraArgs& P, const 
   hipError_t e;
   if (plan.tile == 0) {
     const int grid = helpers + (P.n + 63) / 64 * P.ks;
-    e = P.m <= 16 ? launch<&k_lora_stream<E, 16, 6>>(st, grid, WG, LORA_A_BYTES + 4 * 6 * 2048, P) : launch<&k_lora_stream<E, 32, 6>>(st, grid, WG, LORA_A_BYTES + 4 * 6 * 2048, P);
+    const size_t lds = LORA_A_BYTES + 4 * 6 * 2048;
+    e = P.m <= 16 ? launch<&k_lora_stream<E, 16, 6>>(st, grid, WG, lds, P) : P.m <= 32 ? launch<&k_lora_stream<E, 32, 6>>(st, grid, WG, lds, P) : launch<&k_lora_stream<E, 64, 6>>(st, grid, WG, lds, P);
   } else {
     e = launch<&k_lora_shrink<E>>(st, helpers, LORA_SHRINK_WAVES * 64, (size_t)LORA_SHRINK_WAVES * 16 * P.rp * 4, P, (size_t)LORA_SHRINK_WAVES * 16 * LORA_RMAX * 4);
     if (e != hipSuccess) return e;

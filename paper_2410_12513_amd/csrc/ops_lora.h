@@ -15,7 +15,7 @@
 namespace first {
 
 constexpr int LORA_RMAX = 64;             // largest rank
-constexpr int LORA_STREAM_ROWS = 32;
+constexpr int LORA_STREAM_ROWS = 64;
 
 struct LoraArgs {
   const void *A, *W, *La, *Lb;
@@ -123,7 +123,7 @@ template <typename E> __global__ void __launch_bounds__(LORA_SHRINK_WAVES * 64) 
 // every wave loads its rows of W straight into a ring of its own: it waits for nobody.  Two workgroups a compute unit (80 KB each), 96 KB of W in
 // flight on it.  Partial sums [slice][m][n].
 constexpr int LORA_A_BYTES = 32 * 1024;   // of LDS for the slice of A
-template <typename E, int MR, int S>      // MR: 16 or 32 rows of A; S steps in a wave's ring
+template <typename E, int MR, int S>      // MR: 16, 32 or 64 rows of A; S steps in a wave's ring
 __global__ void __launch_bounds__(WG, 2) k_lora_stream(LoraArgs P) {
   constexpr int RB = 128, EPS = RB / (int)sizeof(E), STG = 16 * RB;
   extern __shared__ __align__(16) char lora_smem[];

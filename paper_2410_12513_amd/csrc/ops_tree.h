@@ -69,18 +69,28 @@ __global__ void __launch_bounds__(QG * KH * 64, QG == 1 ? 1 : 2) k_tree_attn(Tre
   const uint32_t lds0 = (uint32_t)(size_t)(__attribute__((address_space(3))) void*)tree_smem;
   const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)), lane = threadIdx.x & 63, col = lane & 31, gl = lane >> 5;
   const int b = blockIdx.z, split = blockIdx.y, g = blockIdx.x % P.Hkv, G = P.Hq / P.Hkv;
+  const int row0 = blockIdx.x / P.Hkv * (32 * QG), k_lo = split * P.split_keys;
+  // the split's page ids before anybody knows how many of them count: one round trip less ahead of the first keys
+  constexpr int PER = (TREE_SPLIT_MAX / TREE_PAGE + NW * 64 - 1) / (NW * 64);
+  const int last_pg = min((k_lo + P.split_keys) / TREE_PAGE, P.max_pages) - 1;
+  int ids[PER];
+#pragma unroll
+  for (int i = 0; i < PER; ++i) {
+    const int pg = k_lo / TREE_PAGE + (int)threadIdx.x + i * NW * 64;
+    ids[i] = pg <= last_pg ? P.table[(size_t)b * P.max_pages + pg] : -1;
+  }
   const TreeSeq q = tree_seq(P, b);
-  const int rows = q.n * G, row0 = blockIdx.x / P.Hkv * (32 * QG);
-  const int k_lo = split * P.split_keys, k_hi = min(q.len, k_lo + P.split_keys);
+  const int rows = q.n * G, k_hi = min(q.len, k_lo + P.split_keys);
   if (row0 >= rows || (split > 0 && k_lo >= q.len)) return;
   const int n_tree = split == 0 ? (q.n + TK - 1) / TK : 0, n_tiles = n_tree + max(0, k_hi - k_lo + TK - 1) / TK;
   const int n_pg = max(0, k_hi - k_lo + TREE_PAGE - 1) / TREE_PAGE;
   bool hole = false;
-  for (int i = threadIdx.x; i < n_pg; i += NW * 64) {
-    const int id = P.table[(size_t)b * P.max_pages + k_lo / TREE_PAGE + i];
-    const bool ok = id >= 0 && id < P.n_pages;
-    pages[i] = ok ? id : -1;
-    hole |= !ok;
+#pragma unroll
+  for (int i = 0; i < PER; ++i) {
+    const int pg = (int)threadIdx.x + i * NW * 64;
+    const bool ok = ids[i] >= 0 && ids[i] < P.n_pages;
+    if (pg < n_pg) pages[pg] = ok ? ids[i] : -1;
+    hole |= pg < n_pg && !ok;
   }
   const bool holes = __syncthreads_or(hole);
 
@@ -160,7 +170,7 @@ __global__ void __launch_bounds__(QG * KH * 64, QG == 1 ? 1 : 2) k_tree_attn(Tre
 #pragma unroll
       for (int r = 0; r < 16; ++r) W[u][r] = 0.f;
     {                                                      // (fragments requested in two halves ahead of the products: one by one, each product waited for its own)
-      constexpr int H = sizeof(E) == 4 ? 2 : KS / 2;
+      constexpr int H = sizeof(E) == 4 ? (NS == 2 ? 1 : 2) : NS == 2 ? 2 : KS / 2;
       u32x4_t kf[2][H][NS];
       auto fetch = [&](int h) __attribute__((always_inline)) {
 #pragma unroll
@@ -224,8 +234,7 @@ __global__ void __launch_bounds__(QG * KH * 64, QG == 1 ? 1 : 2) k_tree_attn(Tre
     l += (ls[0] + ls[1]) + (ls[2] + ls[3]);
     if constexpr (sizeof(E) == 2) {
       // k-step s2 of a block: keys 16 s2 + 4 gl + 0..3 and 8 more, the rows of registers 8 s2 .. 8 s2 + 7
-#pragma unroll
-      for (int s2 = 0; s2 < 2 * NS; ++s2) {
+      auto values = [&](int s2) __attribute__((always_inline)) {
         union { uint32_t w[4]; u32x4_t x; } ph, pl;
         const int row = kh * NS * 32 + 16 * s2 + 4 * gl + ((lane & 15) >> 2);
         u32x4_t vf[DT];
@@ -244,7 +253,9 @@ __global__ void __launch_bounds__(QG * KH * 64, QG == 1 ? 1 : 2) k_tree_attn(Tre
         for (int d = 0; d < DT; ++d) tree_mma(E{}, O[d], vf[d], pl.x);
 #pragma unroll
         for (int d = 0; d < DT; ++d) tree_mma(E{}, O[d], vf[d], ph.x);
-      }
+      };
+#pragma unroll
+      for (int s2 = 0; s2 < 2 * NS; ++s2) values(s2);
     } else {
 #pragma unroll
       for (int u = 0; u < NS; ++u)
@@ -293,13 +304,15 @@ __global__ void __launch_bounds__(QG * KH * 64, QG == 1 ? 1 : 2) k_tree_attn(Tre
   };
 
 #pragma unroll
-  for (int t = 0; t < S - 1; ++t)
+  for (int t = 0; t < S; ++t)
     if (t < n_tiles) issue(t, t);
   int slot = 0;
-  auto arrived = [&](int t) __attribute__((always_inline)) {          // tile t is there; the tile S - 1 ahead is requested
-    if (t + S - 2 < n_tiles) pg_wait<2 * NI * (S - 2)>(); else pg_wait<0>();
+  auto arrived = [&](int t) __attribute__((always_inline)) {          // tile t is there; the tile S - 1 ahead goes where t - 1 was
+    if (t == 0 && S <= n_tiles) pg_wait<2 * NI * (S - 1)>();
+    else if (t > 0 && t + S - 2 < n_tiles) pg_wait<2 * NI * (S - 2)>();
+    else pg_wait<0>();
     lds_barrier();
-    if (t + S - 1 < n_tiles) issue(t + S - 1, slot == 0 ? S - 1 : slot - 1);
+    if (t > 0 && t + S - 1 < n_tiles) issue(t + S - 1, slot == 0 ? S - 1 : slot - 1);
     const char* at = tree_smem + slot * STG;
     slot = slot + 1 == S ? 0 : slot + 1;
     return at;
@@ -374,12 +387,8 @@ __global__ void __launch_bounds__(WG) k_tree_join(TreeArgs P) {
   if (row >= q.n * P.Hq) return;
   const size_t orow = (size_t)q.o0 * P.Hq + row, all = (size_t)P.N * P.Hq;
   const int ns = max(1, (q.len + P.split_keys - 1) / P.split_keys);
-  float M = -INFINITY;
-  for (int s = lane; s < ns; s += 64) M = fmaxf(M, P.ml[(s * all + orow) * 2]);
-  M = wave_max(M);
-  const float use = M == -INFINITY ? 0.f : M;
-  float o[DL] = {}, L = 0.f;
-  for (int s0 = 0; s0 < ns; s0 += 4) {                     // four splits requested together
+  float M = -INFINITY, o[DL] = {}, L = 0.f;
+  for (int s0 = 0; s0 < ns; s0 += 4) {                     // four splits requested together, and joined as they come
     float2 ml[4];
     float x[4][DL];
 #pragma unroll
@@ -389,6 +398,14 @@ __global__ void __launch_bounds__(WG) k_tree_join(TreeArgs P) {
 #pragma unroll
       for (int e = 0; e < DL; ++e) x[u][e] = P.part[at * HD + lane * DL + e];
     }
+    float top = M;
+#pragma unroll
+    for (int u = 0; u < 4; ++u) top = fmaxf(top, ml[u].x);
+    const float use = top == -INFINITY ? 0.f : top, c0 = __builtin_amdgcn_exp2f(M - use);
+    M = top;
+    L *= c0;
+#pragma unroll
+    for (int e = 0; e < DL; ++e) o[e] *= c0;
 #pragma unroll
     for (int u = 0; u < 4; ++u)
       if (s0 + u < ns) {
