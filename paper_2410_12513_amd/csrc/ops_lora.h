@@ -48,12 +48,12 @@ __device__ __forceinline__ void lora_mma16(float, floatx4_t& acc, u32x4_t a, u32
 template <int RB> __device__ __forceinline__ int lora_slot(int row, int c) { return RB == 128 ? c ^ ((row >> 1) & 7) : c ^ ((row >> 2) & 3); }
 
 // ---- T ---------------------------------------------------------------------------------------------------------------------
-// A workgroup takes 16 rows and every ways-th of the adapters among them; its waves share K out in steps of 64 bytes a row, and their sums meet in LDS.
+// A workgroup takes 16 rows and every ways-th of the adapters among them; its waves share K out in steps of 128 bytes a row, and their sums meet in LDS.
 // Rows without an adapter get their zeros from way 0.  red: NW * 16 * rp floats.
 template <typename E, int NW, int NP>     // NP: blocks of 16 ranks, all of them (rp = 16 NP)
 __device__ __forceinline__ void lora_shrink(const LoraArgs& P, int tile, int way, float* red) {
   constexpr int EPC = 16 / (int)sizeof(E), RP = 16 * NP;   // elements of a chunk
-  constexpr int U = NP == 1 ? 8 : NP == 2 ? 4 : 2;         // steps of a wave requested together
+  constexpr int U = NP == 1 ? 8 : NP == 2 ? 4 : 2;         // half steps of a wave requested together
   const int wave = lora_uni((int)(threadIdx.x >> 6)), lane = threadIdx.x & 63, row = lane & 15, quarter = lane >> 4;
   const int m0 = tile * 16, mr = min(m0 + row, P.m - 1);
   const int id = P.adapter[mr];
@@ -64,7 +64,7 @@ __device__ __forceinline__ void lora_shrink(const LoraArgs& P, int tile, int way
       if (m0 + i / RP < P.m && (a < 0 || a >= P.adapters)) P.T[(size_t)at * RP + i % RP] = 0.f;
     }
   unsigned long long todo = __ballot(have) & 0xffffull;
-  const int steps = (P.k + 4 * EPC - 1) / (4 * EPC);
+  const int steps = (P.k + 8 * EPC - 1) / (8 * EPC);
   const E* x = reinterpret_cast<const E*>(P.A) + (size_t)mr * P.k;
   for (int nth = 0; todo != 0; ++nth) {
     const int a = __builtin_amdgcn_readlane(id, __ffsll(todo) - 1);
@@ -75,11 +75,11 @@ __device__ __forceinline__ void lora_shrink(const LoraArgs& P, int tile, int way
 #pragma unroll
     for (int p = 0; p < NP; ++p) acc[p] = floatx4_t{0.f, 0.f, 0.f, 0.f};
     const E* la = reinterpret_cast<const E*>(P.La) + (size_t)a * P.r * P.k;
-    for (int s0 = wave; s0 < steps; s0 += U * NW) {
+    for (int s0 = wave; s0 < steps; s0 += U / 2 * NW) {
       u32x4_t xa[U], w[U][NP];
 #pragma unroll
-      for (int u = 0; u < U; ++u) {
-        const int at = (s0 + u * NW) * 4 * EPC + quarter * EPC;
+      for (int u = 0; u < U; ++u) {                        // (both halves of a line by the same wave)
+        const int at = (s0 + u / 2 * NW) * 8 * EPC + (2 * quarter + u % 2) * EPC;
         const bool ok = at < P.k;
         xa[u] = ok ? *reinterpret_cast<const u32x4_t*>(x + at) : u32x4_t{0, 0, 0, 0};
 #pragma unroll
