@@ -113,18 +113,19 @@ template <typename E> hipError_t launch_lora(hipStream_t st, LoraArgs& P, const 
 
 // ---- attention of drafted tokens -------------------------------------------------------------------------------------------
 // Rows of a workgroup: the smallest block that holds a sequence's nodes times the query heads of a KV head, up to 256, as its keys are then
-// read once.  Splits: as many as fill the chip's places for workgroups once (by LDS: two a compute unit up to 80 KB, else one), of whole 128 keys.
+// read once.  Splits: as many as fill the chip's places for workgroups once (by LDS: two a compute unit up to 80 KB, else one), of whole 128 keys (fp32: 64, whose products take the matrix cores four times as long a bit).
 struct TreePlan { int block, split_keys, splits, row_blocks; };
 TreePlan tree_plan(const first_tree_attn_desc& d, int B, int max_nodes, int max_len) {
   const int64_t rows = (int64_t)max_nodes * (d.n_q_heads / d.n_kv_heads);
   const bool wide = d.dtype == FIRST_DTYPE_BF16;
   TreePlan p;
-  p.block = rows <= 32 ? 32 : wide && rows <= 64 ? 64 : !wide || rows <= 128 ? 128 : 256;
+  p.block = rows <= 32 ? 32 : rows <= 64 ? 64 : !wide || rows <= 128 ? 128 : 256;
   p.row_blocks = (int)((rows + p.block - 1) / p.block);
   const int places = CUS * (wide && (p.block == 64 || p.block == 128 || d.head_dim == 64) ? 2 : 1);
   const int64_t base = std::max<int64_t>(1, (int64_t)B * d.n_kv_heads * p.row_blocks);
   const int64_t want = std::max<int64_t>(1, places / base);
-  p.split_keys = (int)std::min<int64_t>(TREE_SPLIT_MAX, std::max<int64_t>(128, up((max_len + want - 1) / want, 128)));
+  const int least = wide ? 128 : 64;
+  p.split_keys = (int)std::min<int64_t>(TREE_SPLIT_MAX, std::max<int64_t>(least, up((max_len + want - 1) / want, least)));
   p.splits = std::max(1, (max_len + p.split_keys - 1) / p.split_keys);
   return p;
 }
@@ -137,7 +138,8 @@ template <typename E, int HD> hipError_t launch_tree(hipStream_t st, const TreeA
     e = p.block == 32 ? launch_tree_walk<E, HD, 1, 4, 1, 2>(st, P, p) : p.block == 64 ? launch_tree_walk<E, HD, 2, 2, 1, 2>(st, P, p)
         : p.block == 128 ? launch_tree_walk<E, HD, 4, 1, 2, 2>(st, P, p) : launch_tree_walk<E, HD, 8, 1, 2, 3>(st, P, p);
   } else {
-    e = p.block == 32 ? launch_tree_walk<E, HD, 1, 2, 1, 2>(st, P, p) : launch_tree_walk<E, HD, 4, 1, 2, 2>(st, P, p);
+    e = p.block == 32 ? launch_tree_walk<E, HD, 1, 2, 1, 2>(st, P, p) : p.block == 64 ? launch_tree_walk<E, HD, 2, 2, 1, 2>(st, P, p)
+                                                                                        : launch_tree_walk<E, HD, 4, 2, 1, 2>(st, P, p);
   }
   if (e == hipSuccess && p.splits > 1) {
     e = launch<&k_tree_join<E, HD>>(st, dim3((P.max_nodes * P.Hq + WAVES - 1) / WAVES, P.B), WG, 0, P);

@@ -47,6 +47,31 @@ __device__ __forceinline__ void lora_mma16(float, floatx4_t& acc, u32x4_t a, u32
 // place of a row's 16-byte chunk in LDS: rows of 128 bytes (two rows are all banks), and of 64 (four are)
 template <int RB> __device__ __forceinline__ int lora_slot(int row, int c) { return RB == 128 ? c ^ ((row >> 1) & 7) : c ^ ((row >> 2) & 3); }
 
+// Ranks p0 .. of a row of Lb that begins at element `at`, a chunk of them; zeros from rank r on, whatever stands there (the next row: not multiplied even
+// by 0).  One load where the chunk lies inside the array (rows of odd ranks begin anywhere; loads from global memory need no alignment), else one by one.
+template <typename E> __device__ __forceinline__ u32x4_t lora_ranks(const E* lb, size_t at, size_t total, int p0, int r) {
+  constexpr int EPC = 16 / (int)sizeof(E);
+  union { E e[EPC]; u32x4_t v; } f;
+  f.v = u32x4_t{0, 0, 0, 0};
+  const int left = r - p0;
+  if (left <= 0) return f.v;
+  if (at + p0 + EPC <= total) {
+    __builtin_memcpy(&f.v, lb + at + p0, 16);
+    if (left < EPC)
+#pragma unroll
+      for (int d = 0; d < 4; ++d) {
+        constexpr int PER = 4 / (int)sizeof(E);            // elements of a word
+        const int n = left - d * PER;
+        f.v[d] = n >= PER ? f.v[d] : n <= 0 ? 0u : f.v[d] & 0xffffu;
+      }
+    return f.v;
+  }
+#pragma unroll
+  for (int e = 0; e < EPC; ++e)
+    if (e < left) f.e[e] = lb[at + p0 + e];
+  return f.v;
+}
+
 // ---- T ---------------------------------------------------------------------------------------------------------------------
 // A workgroup takes 16 rows and every ways-th of the adapters among them; its waves share K out in steps of 128 bytes a row, and their sums meet in LDS.
 // Rows without an adapter get their zeros from way 0.  red: NW * 16 * rp floats.
@@ -198,17 +223,12 @@ __global__ void __launch_bounds__(WG) k_lora_finish(LoraArgs P) {
   for (int u = 0; u < P.ks; ++u) s += P.part[((size_t)u * P.m + row) * P.n + col];
   if (a >= 0 && a < P.adapters) {
     const float* t = P.T + (size_t)row * P.rp;
-    const E* lb = reinterpret_cast<const E*>(P.Lb) + ((size_t)a * P.n + col) * P.r;
+    const size_t at = ((size_t)a * P.n + col) * P.r, all = (size_t)P.adapters * P.n * P.r;
     float d = 0.f;
-    if (P.r % EPC == 0) {
-      for (int p = 0; p < P.r; p += EPC) {
-        float x[EPC];
-        load_vec(lb + p, x);
+    for (int p = 0; p < P.r; p += EPC) {
+      union { u32x4_t v; E e[EPC]; } w = {lora_ranks(reinterpret_cast<const E*>(P.Lb), at, all, p, P.r)};
 #pragma unroll
-        for (int e = 0; e < EPC; ++e) d = fmaf(t[p + e], x[e], d);
-      }
-    } else {
-      for (int p = 0; p < P.r; ++p) d = fmaf(t[p], to_f32(lb[p]), d);
+      for (int e = 0; e < EPC; ++e) d = fmaf(t[p + e], to_f32(w.e[e]), d);
     }
     s += d;
   }
@@ -292,75 +312,84 @@ __global__ void __launch_bounds__(WGM * WGN * 64, 1) k_lora_tile(LoraArgs P) {
     if (s0 + s < s1) issue(s0 + s, s);
 
   if (P.ks == 1) {
-    // The second product first, while the first tiles are on their way: the adapters among 64 of this wave's rows, one after the other, all that a step of
-    // two chunks of ranks needs of an adapter requested together.
+    // The second product first, while the first tiles are on their way: for 64 of this wave's rows at a time the adapters among them, one after the other, in steps of
+    // two chunks of ranks.  What a step needs is requested while the one before it is multiplied: rows of many adapters were as many round trips in a row.
     constexpr int H = IM < 2 ? IM : 2;
+    struct Step { unsigned long long rows; u32x4_t w[JN], t[H][EPC / 4]; };
 #pragma unroll
     for (int h = 0; h < IM / H; ++h) {
       const int mine = m0 + wm + 64 * h + min(lane, TM - 1), ad = P.adapter[min(mine, P.m - 1)];
-      unsigned long long todo = __ballot(lane < TM && mine < P.m && ad >= 0 && ad < P.adapters);
-      while (todo != 0) {
-        const int a = __builtin_amdgcn_readlane(ad, __ffsll(todo) - 1);
-        const unsigned long long rows = __ballot(ad == a) & todo;
-        todo &= ~rows;
-        const E* const lb = reinterpret_cast<const E*>(P.Lb) + (size_t)a * P.n * P.r;
-        for (int p = 0; p < P.r; p += 2 * EPC) {
-          const int p0 = p + lg * EPC;
-          u32x4_t w[JN], t[H][EPC / 4];
+      unsigned long long todo = __ballot(lane < TM && mine < P.m && ad >= 0 && ad < P.adapters), rows = 0;
+      int a = 0, p = P.r;
+      auto next = [&](Step& st) __attribute__((always_inline)) {
+        if (p >= P.r) {                                    // the next adapter
+          if (todo == 0) return false;
+          a = __builtin_amdgcn_readlane(ad, __ffsll(todo) - 1);
+          rows = __ballot(ad == a) & todo;
+          todo &= ~rows;
+          p = 0;
+        }
+        st.rows = rows;
+        const int p0 = p + lg * EPC;
+        const E* const lb = reinterpret_cast<const E*>(P.Lb);
+#pragma unroll
+        for (int j = 0; j < JN; ++j)
+          st.w[j] = lora_ranks(lb, ((size_t)a * P.n + min(n0 + wn + 32 * j + lr, P.n - 1)) * P.r, (size_t)P.adapters * P.n * P.r, p0, P.r);
+#pragma unroll
+        for (int i = 0; i < H; ++i)
+#pragma unroll
+          for (int e = 0; e < EPC / 4; ++e) {              // (a row of another adapter: zeros; rp is a multiple of two chunks)
+            st.t[i][e] = u32x4_t{0, 0, 0, 0};
+            if (rows >> (32 * i + lr) & 1) st.t[i][e] = *reinterpret_cast<const u32x4_t*>(P.T + (size_t)(m0 + wm + 64 * h + 32 * i + lr) * P.rp + p0 + 4 * e);
+          }
+        p += 2 * EPC;
+        return true;
+      };
+      auto multiply = [&](const Step& st) __attribute__((always_inline)) {
+#pragma unroll
+        for (int i = 0; i < H; ++i) {
+          u32x4_t part[3];
+          if constexpr (sizeof(E) == 2) {
+            float x[EPC];
+#pragma unroll
+            for (int e = 0; e < EPC; ++e) x[e] = __uint_as_float(st.t[i][e / 4][e % 4]);
+#pragma unroll
+            for (int q = 0; q < 3; ++q)
+#pragma unroll
+              for (int e = 0; e < 4; ++e) {
+                part[q][e] = pk_bf16(x[2 * e], x[2 * e + 1]);
+                x[2 * e] -= __uint_as_float(part[q][e] << 16); x[2 * e + 1] -= __uint_as_float(part[q][e] & 0xffff0000u);
+              }
+          }
+          const uint32_t of = (uint32_t)(st.rows >> (32 * i)) >> (4 * lg);
 #pragma unroll
           for (int j = 0; j < JN; ++j) {
-            const E* at = lb + (size_t)min(n0 + wn + 32 * j + lr, P.n - 1) * P.r + p0;
-            w[j] = u32x4_t{0, 0, 0, 0};
-            if (P.r % EPC == 0) {
-              if (p0 < P.r) w[j] = *reinterpret_cast<const u32x4_t*>(at);
-            } else {
-              union { E e[EPC]; u32x4_t v; } f;
-              f.v = w[j];
+            floatx16_t d;
 #pragma unroll
-              for (int e = 0; e < EPC; ++e)
-                if (p0 + e < P.r) f.e[e] = at[e];
-              w[j] = f.v;
-            }
-          }
-#pragma unroll
-          for (int i = 0; i < H; ++i)
-#pragma unroll
-            for (int e = 0; e < EPC / 4; ++e) {            // (a row of another adapter: zeros; rp is a multiple of two chunks)
-              t[i][e] = u32x4_t{0, 0, 0, 0};
-              if (rows >> (32 * i + lr) & 1) t[i][e] = *reinterpret_cast<const u32x4_t*>(P.T + (size_t)(m0 + wm + 64 * h + 32 * i + lr) * P.rp + p0 + 4 * e);
-            }
-#pragma unroll
-          for (int i = 0; i < H; ++i) {
-            u32x4_t part[3];
+            for (int r = 0; r < 16; ++r) d[r] = 0.f;
             if constexpr (sizeof(E) == 2) {
-              float x[EPC];
 #pragma unroll
-              for (int e = 0; e < EPC; ++e) x[e] = __uint_as_float(t[i][e / 4][e % 4]);
-#pragma unroll
-              for (int q = 0; q < 3; ++q)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                  part[q][e] = pk_bf16(x[2 * e], x[2 * e + 1]);
-                  x[2 * e] -= __uint_as_float(part[q][e] << 16); x[2 * e + 1] -= __uint_as_float(part[q][e] & 0xffff0000u);
-                }
+              for (int q = 2; q >= 0; --q) lora_mma32(E{}, d, part[q], st.w[j]);
+            } else {
+              lora_mma32(E{}, d, st.t[i][0], st.w[j]);
             }
-            const uint32_t of = (uint32_t)(rows >> (32 * i)) >> (4 * lg);
 #pragma unroll
-            for (int j = 0; j < JN; ++j) {
-              floatx16_t d;
-#pragma unroll
-              for (int r = 0; r < 16; ++r) d[r] = 0.f;
-              if constexpr (sizeof(E) == 2) {
-#pragma unroll
-                for (int q = 2; q >= 0; --q) lora_mma32(E{}, d, part[q], w[j]);
-              } else {
-                lora_mma32(E{}, d, t[i][0], w[j]);
-              }
-#pragma unroll
-              for (int r = 0; r < 16; ++r) acc[H * h + i][j][r] += of >> (8 * (r >> 2) + (r & 3)) & 1 ? d[r] : 0.f;
-            }
+            for (int r = 0; r < 16; ++r) acc[H * h + i][j][r] += of >> (8 * (r >> 2) + (r & 3)) & 1 ? d[r] : 0.f;
           }
         }
+      };
+      Step one, two;
+      if constexpr (JN > 2) {                              // (two steps' registers are not there beside 64 x 128 accumulators)
+        while (next(one)) multiply(one);
+        continue;
+      }
+      bool more = next(one);
+      while (more) {
+        more = next(two);
+        multiply(one);
+        if (!more) break;
+        more = next(one);
+        multiply(two);
       }
     }
   }

@@ -150,7 +150,7 @@ __device__ inline SrFound sr_find(const float* row, int V, int index_bits, const
 
 // ---- a row in three looks --------------------------------------------------------------------------------------------------
 // What can be drawn and where the cuts lie is decided among a few tokens, a list in LDS that is put in order; what is not on it only matters by its sum.
-//   with top_k (up to SR_TOPK), or few tokens: the k-th largest of the threads' (of groups' of 16 threads) own maxima is a bound that at least k tokens reach; the
+//   with top_k (up to SR_TOPK): the k-th largest of the maxima of threads, or of groups of 2 to 16 of them, is a bound that at least k tokens reach; the
 //     list is what reaches it, and no other weight is formed;
 //   else: a histogram of the masses over 4096 equal parts of the range of logits that weigh anything says in which part each cut lies, and in which few the draw
 //     can lie; the list is those parts' tokens.
@@ -199,7 +199,7 @@ __device__ __forceinline__ unsigned long long sr_key(float l, int i) { return (u
 // list[0 .. n) into descending order, n <= SR_LIST.  Ends with a barrier.
 __device__ inline void sr_sort(unsigned long long* list, int n) {
   const int tid = threadIdx.x;
-  if (n <= 512) {                                          // by rank: a key's place is the number of larger ones (all differ but for zeros)
+  if (n <= 128) {                                          // by rank: a key's place is the number of larger ones (all differ but for zeros)
     const unsigned long long x = tid < n ? list[tid] : 0ull;
     int before = 0;
     if (tid < n)
@@ -211,7 +211,7 @@ __device__ inline void sr_sort(unsigned long long* list, int n) {
     __syncthreads();
     return;
   }
-  int size = 1024;
+  int size = 256;
   while (size < n) size *= 2;
   for (int i = n + tid; i < size; i += SR_THREADS) list[i] = 0ull;
   __syncthreads();
@@ -271,7 +271,7 @@ struct SrFirst { float value; int index; };                // a thread's own lar
 // False: the list did not fit.
 __device__ inline bool sr_fast(const float* row, int V, const SrRow& R, const SrRules& Q, SrFirst first, float lmin, SrFast& sh, SrOut& out) {
   const int tid = threadIdx.x;
-  const bool by_prefix = Q.top_k > 0 && Q.top_k <= SR_TOPK, whole = V <= SR_LIST;
+  const bool by_prefix = Q.top_k > 0 && Q.top_k <= SR_TOPK, whole = V <= 512 || (V <= SR_LIST && Q.top_k > SR_TOPK);      // (512: put in order in one go)
   const bool cut_p = !Q.greedy && Q.top_p < 1.f, cut_m = !Q.greedy && Q.min_p > 0.f;
   if (Q.top_k > SR_TOPK && Q.top_k < V && !whole) return false;
   if (!(whole || by_prefix) && !(R.lmax < INFINITY)) return false;
@@ -281,28 +281,31 @@ __device__ inline bool sr_fast(const float* row, int V, const SrRow& R, const Sr
     unsigned long long bound = 0ull;
     if (!whole) {
       unsigned long long own = first.value > -INFINITY ? sr_key(first.value, first.index) : 0ull;
-      if (Q.top_k <= 64) {                                 // groups of 16 threads
-#pragma unroll
-        for (int d = 8; d > 0; d >>= 1) {
-          const unsigned long long o = (unsigned long long)__shfl_xor((long long)own, d, 64);
-          own = o > own ? o : own;
-        }
-        if ((tid & 15) == 0) sh.list[tid >> 4] = own;
-      } else {
-        sh.list[tid] = own;
+      // groups of g threads: as large as leaves some more groups with tokens than the bound has to count
+      int g = 16;
+      while (g > 1 && (SR_THREADS / g < Q.top_k + Q.top_k / 4 || V / (4 * g) < Q.top_k + Q.top_k / 4)) g /= 2;
+      for (int d = 1; d < g; d *= 2) {
+        const unsigned long long o = (unsigned long long)__shfl_xor((long long)own, d, 64);
+        own = o > own ? o : own;
       }
+      if (tid % g == 0) sh.list[tid / g] = own;
       __syncthreads();
-      sr_sort(sh.list, Q.top_k <= 64 ? 64 : SR_THREADS);   // (the zeros of threads without a token stand behind the others)
+      sr_sort(sh.list, SR_THREADS / g);                    // (the zeros of threads without a token stand behind the others)
       bound = sh.list[Q.top_k - 1];
       __syncthreads();
     }
-    sr_each(row, V, [&](float l, int i) {
-      if (!(l > -INFINITY)) return;
-      const unsigned long long key = sr_key(l, i);
-      if (key < bound) return;
-      const int to = atomicAdd(&sh.found, 1);
-      if (to < SR_LIST) sh.list[to] = key;
-    });
+    if (whole) {                                           // (what is no token: 0, behind the others)
+      for (int i = tid; i < V; i += SR_THREADS) sh.list[i] = row[i] > -INFINITY ? sr_key(row[i], i) : 0ull;
+      if (tid == 0) sh.found = V;
+    } else {
+      sr_each(row, V, [&](float l, int i) {
+        if (!(l > -INFINITY)) return;
+        const unsigned long long key = sr_key(l, i);
+        if (key < bound) return;
+        const int to = atomicAdd(&sh.found, 1);
+        if (to < SR_LIST) sh.list[to] = key;
+      });
+    }
   } else {
     // masses over equal parts of [lmax - range, lmax]; what weighs less than 2^-66 is in the last part
     const float inv = sr_parts(R, lmin);
