@@ -73,6 +73,33 @@ def test_lora_of_long_prompts():
     _lora_check(_lora_inputs(BF, 2049, 520, 264, 24, 32))
 
 
+@pytest.mark.parametrize("dtype", [BF, FP])
+@pytest.mark.parametrize("m,n,k,r,ads", [(100, 130, 4096, 7, 3), (130, 600, 2056, 24, 5), (64, 3000, 128, 40, 2), (40, 64, 8, 64, 1)])
+def test_lora_slices_of_the_contraction(dtype, m, n, k, r, ads):
+    """Few tiles and a long contraction: slices of it, added in order (and what is cut into slices without need)."""
+    _lora_check(_lora_inputs(dtype, m, n, k, r, ads, seed=4))
+    _lora_check(_lora_inputs(dtype, m, n, k, r, ads, seed=5, kind="runs"), accumulate=True)
+
+
+@pytest.mark.parametrize("kind,r", [("runs", 8), ("mixed", 19)])
+def test_lora_large_tiles(kind, r):
+    _lora_check(_lora_inputs(BF, 4000, 4001, 136, r, 6, seed=6, kind=kind), accumulate=kind == "runs")
+
+
+def test_lora_last_ranks_of_the_last_adapter():
+    """Ranks that fill no chunk, at the very end of Lb: the array ends a page, nothing behind it may be read into the result."""
+    import paper_2410_12513_amd as P
+    for r in (1, 3, 9, 13):
+        for m in (4, 50, 300):
+            A, W, La, Lb, ids, scale = _lora_inputs(BF, m, 70, 64, r, 2, seed=r, kind="one")
+            big = torch.full((Lb.numel() + 64,), float("nan"), dtype=BF, device="cuda")
+            big[:Lb.numel()] = Lb.cuda().flatten()
+            C = torch.empty((m, 70), device="cuda")
+            P.op_gemm_nt_lora(A.cuda(), W.cuda(), La.cuda(), big[:Lb.numel()].view(Lb.shape), ids.cuda(), scale.cuda(), C)
+            ref, size = F.lora(A, W, La, Lb, ids, scale)
+            assert bool(((C.cpu().double() - ref).abs() <= 2e-6 * size).all())
+
+
 def test_lora_rows_do_not_depend_on_their_neighbours_adapters():
     """Infinities in an adapter stay with its own rows, and no adapter reads a row that is not its."""
     import paper_2410_12513_amd as P
@@ -144,6 +171,12 @@ def test_rope(dtype, layout, rows, heads, hd, rot):
 def test_rope_scalings_and_the_way_back(dtype, scaling):
     _rope_check(dtype, 65, 4, 128, 128, "half", scaling, base=500000.0)
     _rope_check(dtype, 65, 4, 128, 96, "interleaved", scaling, inverse=True, amplitude=1.25, packed=6)
+
+
+@pytest.mark.parametrize("dtype", [BF, FP])
+@pytest.mark.parametrize("layout", ["half", "interleaved"])
+def test_rope_of_long_prompts(dtype, layout):
+    _rope_check(dtype, 8195, 2, 64, 48, layout, packed=3, inplace=True)
 
 
 def test_rope_positions_of_any_size():
@@ -261,6 +294,52 @@ def test_tree_attention_over_long_caches(dtype, hd):
     _tree_compare(t, *_tree_run(t))
 
 
+def test_tree_splits_of_the_largest_size():
+    """So many heads that a sequence is cut into splits of the largest size only; the others are short."""
+    t = _tree_inputs(BF, [8300, 0, 3, 17, 5, 1, 40, 16], [1, 1, 2, 1, 0, 1, 1, 1], 64, 64, 64, seed=12)
+    _tree_compare(t, *_tree_run(t))
+
+
+def test_tree_pages_far_into_a_large_cache():
+    """Pages whose elements lie past 2^31."""
+    import paper_2410_12513_amd as P
+    t = _tree_inputs(BF, [100, 33], [5, 2], 32, 8, 128, seed=14)
+    n, per = t["pool"].shape[0], t["pool"][0].numel()
+    far = 2 ** 31 // per + 9
+    big = torch.empty((far + n, *t["pool"].shape[1:]), dtype=BF, device="cuda")
+    big[far:] = t["pool"].cuda()
+    d = {k: v.cuda() for k, v in t.items() if k != "pool"}
+    table = torch.where(d["table"] < n, d["table"] + far, d["table"])
+    out, lse = torch.full_like(d["q"], 7.0), torch.full(d["q"].shape[:2], 7.0, device="cuda")
+    P.op_tree_attn(d["q"], d["k"], d["v"], big, table, d["lens"], d["offs"], out, 5, 100, mask=d["mask"], lse=lse)
+    _tree_compare(t, out, lse)
+
+
+def test_tree_sequences_that_share_pages():
+    t = _tree_inputs(BF, [64, 64, 50], [3, 2, 4], 8, 2, 64, seed=15)
+    t["table"][1] = t["table"][0]
+    t["table"][2, :3] = t["table"][0, 0]
+    t["pool"] = torch.nan_to_num(t["pool"].float(), 0, 0, 0).to(BF)
+    _tree_compare(t, *_tree_run(t))
+
+
+@pytest.mark.parametrize("scale", [0.0, -0.2, 1.0])
+def test_tree_scales(scale):
+    for dtype in (BF, FP):
+        t = _tree_inputs(dtype, [40, 9], [3, 6], 4, 2, 64, seed=16, masks="some")
+        _tree_compare(t, *_tree_run(t, scale=scale), scale=scale)
+
+
+def test_tree_masks_of_infinite_scores():
+    """Keys of the largest values: scores beyond 32 bits of some nodes are infinite, and only their own rows feel it."""
+    t = _tree_inputs(FP, [20], [6], 2, 1, 64, seed=17)
+    t["k"][2] = 3e38
+    t["mask"][:, 0] &= ~(1 << 2)
+    out, lse = _tree_run(t)
+    assert bool(torch.isfinite(out).all()) and bool(torch.isfinite(lse).all())
+    _tree_compare({**t, "k": t["k"].clamp(max=3.0)}, out, lse)
+
+
 def test_tree_bounds_shorter_than_the_sequences():
     """max_len, max_nodes and the page table's width cut what the device's numbers say; rows past max_nodes stay as they were."""
     t = _tree_inputs(BF, [100, 40], [9, 4], 4, 2, 64, seed=3)
@@ -344,6 +423,34 @@ def _logits(rows, vocab, seed=0, std=2.0):
 def test_sample(vocab, rules):
     rng = np.random.default_rng(vocab)
     _sample_check(_logits(9, vocab, vocab), rng.random(9), **rules)
+
+
+@pytest.mark.parametrize("vocab", [600, 5000, 32000, 128256])
+@pytest.mark.parametrize("rules", [{"top_p": 0.95, "min_p": 0.01}, {"top_p": 0.3, "min_p": 1e-4}, {"top_k": 2000}, {"top_k": 500, "top_p": 0.9}, {"top_k": 100, "min_p": 1e-3},
+                                   {"top_p": 0.999999}, {"min_p": 1e-20}, {"temperature": 0.05}, {"temperature": 0.05, "top_p": 0.99}, {"temperature": 1e4, "top_p": 0.5},
+                                   {"min_p": 1.0}, {"min_p": 0.999}])
+def test_sample_cuts(vocab, rules):
+    rng = np.random.default_rng(vocab + 1)
+    _sample_check(_logits(5, vocab, vocab + 1, 1.0), rng.random(5), least=0.6, **rules)
+
+
+@pytest.mark.parametrize("rules", [{}, {"top_p": 0.6}, {"min_p": 0.5}, {"top_k": 700, "top_p": 0.8}])
+def test_sample_crowded_logits(rules):
+    """Logits so near each other that parts of the range hold thousands, and one far away that stretches it."""
+    rng = np.random.default_rng(21)
+    l = (rng.normal(size=(6, 60000)) * 1e-3).astype(np.float32)
+    l[1, 7], l[2, 59999] = 30.0, 5.0
+    l[3] *= 50
+    l[4, ::2] = -1e30
+    l[5] = l[5].astype(np.float16).astype(np.float32)
+    _sample_check(l, rng.random(6), least=0.6, **rules)
+
+
+def test_sample_many_rows_and_a_large_vocabulary():
+    rng = np.random.default_rng(22)
+    _sample_check(_logits(300, 700, 23), rng.random(300), temperature=0.9, top_p=0.9)
+    _sample_check(_logits(2, 1000003, 24), rng.random(2), temperature=0.9, top_p=0.9)
+    _sample_check(_logits(2, 1000003, 25), rng.random(2), top_k=50)
 
 
 def test_sample_rules_of_rows():
