@@ -411,6 +411,15 @@ int first_op_tree_attn(void *hip_stream, const first_tree_attn_desc *desc, const
                        const uint64_t *tree_mask, void *out, float *lse, int32_t B, int32_t N, int32_t max_nodes, int32_t max_len,
                        void *workspace, int64_t workspace_bytes);
 
+/* first_op_tree_attn over the cache of a context: sequence b is the b-th live one, with all positions that it holds, on the context's stream; dtype, heads, pages and
+ * scale (1 / sqrt(head_dim)) are the model's.  A layer that a sequence skips holds nothing of its decoded positions (Section 4.3 item 2): give such a sequence no
+ * nodes.  Nothing enters the cache; what is accepted goes there through first_kv_write or the next decode steps.  FIRST_ERR_STATE when no sequence is live or no live sequence
+ * stored the layer's KV; FIRST_ERR_ARG where the pages are not of 16 tokens.  workspace: first_tree_attn_workspace bytes for the lengths at the call. */
+int64_t first_tree_attn_workspace(first_ctx *ctx, int32_t N, int32_t max_nodes);
+int first_tree_attn(first_ctx *ctx, int32_t layer, const void *q, const void *k_new, const void *v_new, const int32_t *node_offsets,
+                    const uint64_t *tree_mask, int32_t mask_words, void *out, float *lse, int32_t N, int32_t max_nodes, void *workspace,
+                    int64_t workspace_bytes);
+
 /* Tokens drawn from rows of logits, each row by rules of its own; the draws are the caller's, as in first_sample_top_k.  The tokens of
  * a row stand in order of their logits, largest first, equal ones by index; a token weighs w = exp((l - l_max) / temperature).  Each rule keeps a prefix
  * of that order and the shortest is kept:

@@ -19,7 +19,7 @@ EXPORTS = ["first_create", "first_destroy", "first_prefill_route", "first_set_ma
            "first_num_pages", "first_op_gemv", "first_op_gemm_nt", "first_op_gateup", "first_step_timing", "first_op_gemm_nt_f32a", "first_set_seq_len", "first_kv_usage", "first_soft_forward",
            "first_lora_merge", "first_sample_top_k_static", "first_decode_step_sampled",
            "first_op_gemm_nt_lora", "first_op_gemm_nt_lora_workspace", "first_op_rope", "first_op_tree_attn",
-           "first_op_tree_attn_workspace", "first_sample", "first_sample_workspace"]
+           "first_op_tree_attn_workspace", "first_sample", "first_sample_workspace", "first_tree_attn", "first_tree_attn_workspace"]
 ROPE_LAYOUTS = {"half": 0, "interleaved": 1}
 ROPE_SCALINGS = {"none": 0, "linear": 1, "bands": 2}
 
@@ -81,6 +81,7 @@ def load_library():
         for name, args in (("first_op_gemm_nt_lora", (p, i, p, p, p, p, p, p, p, i, i, i, i, i, i, p, l)),
                            ("first_op_gemm_nt_lora_workspace", (i,) * 5), ("first_op_rope", (p, p, p, l, p, l, p, i)),
                            ("first_op_tree_attn", (p,) * 12 + (i,) * 4 + (p, l)), ("first_op_tree_attn_workspace", (p,) + (i,) * 4),
+                           ("first_tree_attn", (p, i, p, p, p, p, p, i, p, p, i, i, p, l)), ("first_tree_attn_workspace", (p, i, i)),
                            ("first_sample", (p, p, l, i, i) + (p,) * 8 + (p, l)), ("first_sample_workspace", (i, i))):
             getattr(lib, name).argtypes = args
             if name.endswith("_workspace"):
@@ -268,6 +269,24 @@ class FirstContext:
             _check_dev(candidates_out, torch.int32, "candidates_out", B * top_k)
         self._chk(self.lib.first_sample_top_k(self.h, _ptr(logits), _ptr(uniforms), C.c_float(temperature),
                                               C.c_int32(top_k), _ptr(token_out), _ptr(candidates_out)))
+
+    def tree_attn(self, layer: int, q: torch.Tensor, k_new: torch.Tensor, v_new: torch.Tensor, node_offsets: torch.Tensor, out: torch.Tensor, max_nodes: int,
+                  mask: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None) -> None:
+        """op_tree_attn of drafted tokens over the live sequences' cache of one layer, on the context's stream.  The workspace (None: one of this call's) must
+        live until that stream is through with it."""
+        desc, dev = self.desc, _device(q)
+        dtype = torch.bfloat16 if desc.dtype == "bf16" else torch.float32
+        N, hq, hkv, hd, words = q.shape[0], desc.n_q_heads, desc.n_kv_heads, desc.head_dim, 0 if mask is None else mask.shape[1]
+        ptrs = (_same(q, dtype, (N, hq, hd), dev, "q"), _same(k_new, dtype, (N, hkv, hd), dev, "k_new"), _same(v_new, dtype, (N, hkv, hd), dev, "v_new"),
+                _same(node_offsets, torch.int32, (self.batch() + 1,), dev, "node_offsets"), 0 if mask is None else _same(mask, torch.int64, (N, words), dev, "mask"))
+        outs = (_same(out, dtype, (N, hq, hd), dev, "out"), 0 if lse is None else _same(lse, torch.float32, (N, hq), dev, "lse"))
+        if workspace is None:
+            need = self.lib.first_tree_attn_workspace(self.h, N, max_nodes)
+            if need < 0:
+                self._chk(int(need))
+            workspace = torch.empty(max(1, need), dtype=torch.uint8, device=f"cuda:{dev}")
+            workspace.record_stream(self.stream or torch.cuda.default_stream(dev))
+        self._chk(self.lib.first_tree_attn(self.h, layer, *ptrs, words, *outs, N, max_nodes, workspace.data_ptr(), workspace.numel() * workspace.element_size()))
 
     def get_hidden(self) -> torch.Tensor:
         out = torch.empty((self.batch(), self.desc.d_model), dtype=torch.float32, device="cuda")

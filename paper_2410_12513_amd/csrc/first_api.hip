@@ -1948,6 +1948,37 @@ int first_kv_write(first_ctx* c, int32_t seq, int32_t layer, int32_t pos0, int32
   return kv_tap(c, seq, layer, pos0, n, const_cast<float*>(k_in), const_cast<float*>(v_in), true);
 }
 
+static first_tree_attn_desc tree_desc_of(const first_ctx* c, int mask_words) {
+  return {c->d.dtype, c->d.n_q_heads, c->d.n_kv_heads, c->d.head_dim, c->d.kv_page_tokens, c->n_pages, c->max_pages, mask_words, 1.0f / std::sqrt((float)c->d.head_dim)};
+}
+static int longest(const first_ctx* c) {
+  int most = 0;
+  for (int b = 0; b < c->B; ++b) most = std::max(most, c->hlen[b]);
+  return most;
+}
+
+int64_t first_tree_attn_workspace(first_ctx* c, int32_t N, int32_t max_nodes) {
+  if (!c) return FIRST_ERR_ARG;
+  if (c->B < 1) return fail(c, FIRST_ERR_STATE, "first_tree_attn: no live sequence");
+  const first_tree_attn_desc d = tree_desc_of(c, 0);
+  const int64_t need = first_op_tree_attn_workspace(&d, c->B, N, max_nodes, longest(c));
+  return need >= 0 ? need : fail(c, (int)need, g_create_error);
+}
+
+int first_tree_attn(first_ctx* c, int32_t layer, const void* q, const void* k_new, const void* v_new, const int32_t* node_offsets, const uint64_t* tree_mask,
+                    int32_t mask_words, void* out, float* lse, int32_t N, int32_t max_nodes, void* workspace, int64_t workspace_bytes) {
+  if (!c) return FIRST_ERR_ARG;
+  if (c->B < 1) return fail(c, FIRST_ERR_STATE, "first_tree_attn: no live sequence");
+  if (layer < 0 || layer >= c->d.n_layers) return fail(c, FIRST_ERR_ARG, "first_tree_attn: layer out of range");
+  bool stored = false;
+  for (int b = 0; b < c->B; ++b) stored |= c->has_kv[b][layer] != 0;
+  if (!stored) return fail(c, FIRST_ERR_STATE, "first_tree_attn: the KV of this layer was not stored (kv_layer_slots)");
+  const first_tree_attn_desc d = tree_desc_of(c, mask_words);
+  const int rc = first_op_tree_attn(c->stream, &d, q, k_new, v_new, kv_base(c, layer), c->d_page_table, c->d_len, node_offsets, tree_mask, out, lse, c->B, N, max_nodes,
+                                    longest(c), workspace, workspace_bytes);
+  return rc == FIRST_OK ? rc : fail(c, rc, g_create_error);
+}
+
 int first_set_seq_len(first_ctx* c, int32_t seq, int32_t len) {
   if (!c) return FIRST_ERR_ARG;
   if (seq < 0 || seq >= c->B) return fail(c, FIRST_ERR_STATE, "first_set_seq_len: no such live sequence");

@@ -379,11 +379,51 @@ def test_tree_without_a_cache():
     _tree_compare(t, out, lse)
 
 
-def test_tree_one_node_is_a_decode_step_over_a_contexts_cache():
-    """The page layout is that of the contexts: pages written by hand in the order of a context's pool."""
-    t = _tree_inputs(BF, [70], [1], 4, 2, 64, masks="chain")
-    t["mask"] = None
-    _tree_compare(t, *_tree_run(t))
+@pytest.mark.parametrize("model", ["mini_bf16", "tiny"])
+def test_tree_attention_over_the_cache_of_a_context(model):
+    """The pages, tables and lengths of live sequences, in a shuffled page order, before and after decode steps."""
+    import paper_2410_12513_amd as P
+    from synth import CONFIGS, make_prompt, make_router, make_weights
+    from synth.generators import to_device
+    desc = CONFIGS[model]
+    dtype, hq, hkv, hd = (BF if desc.dtype == "bf16" else FP), desc.n_q_heads, desc.n_kv_heads, desc.head_dim
+    ctx = P.FirstContext(desc, to_device(make_weights(desc, 5), "cuda"), make_router(desc, 5).cuda(), max_batch=3, max_seq_len=96)
+    with pytest.raises(P.FirstError) as e:                   # no live sequence
+        one = torch.zeros(1, hq, hd, dtype=dtype, device="cuda")
+        ctx.tree_attn(0, one, torch.zeros(1, hkv, hd, dtype=dtype, device="cuda"), torch.zeros(1, hkv, hd, dtype=dtype, device="cuda"),
+                      torch.zeros(1, dtype=torch.int32, device="cuda"), one.clone(), 1)
+    assert e.value.code == -2
+    order = list(range(ctx.num_pages()))
+    random.Random(3).shuffle(order)
+    ctx.set_page_order(order)
+    lens = [40, 16, 1]
+    ctx.prefill_route(torch.cat([make_prompt(desc.vocab, n, 60 + n) for n in lens]).cuda(), lens)
+    for b in range(3):
+        ctx.set_mask(b, [1] * desc.n_layers)
+    t = _tree_inputs(dtype, [0, 0, 0], [5, 1, 3], hq, hkv, hd, seed=18)
+    d = {k: t[k].cuda() for k in ("q", "k", "v", "offs", "mask")}
+    tok = torch.tensor([1, 2, 3], dtype=torch.int32, device="cuda")
+    for step in range(3):
+        layer = desc.n_layers - 1 if step else 0
+        out, lse = torch.full_like(d["q"], 7.0), torch.full(d["q"].shape[:2], 7.0, device="cuda")
+        ctx.tree_attn(layer, d["q"], d["k"], d["v"], d["offs"], out, 5, mask=d["mask"], lse=lse)
+        ctx.sync()
+        now = [ctx.seq_len(b) for b in range(3)]
+        assert now == [n + step for n in lens]
+        pages = [-(-n // 16) for n in now]
+        pool, table, at = torch.zeros((sum(pages), 2, hkv, 16, hd), dtype=dtype), torch.zeros((3, max(pages)), dtype=torch.int32), 0
+        for b, n in enumerate(now):
+            k, v = ctx.kv_read(b, layer, 0, n)
+            for p in range(n):
+                pool[at + p // 16, 0, :, p % 16], pool[at + p // 16, 1, :, p % 16] = k[p].cpu().to(dtype), v[p].cpu().to(dtype)
+            table[b, :pages[b]] = torch.arange(at, at + pages[b])
+            at += pages[b]
+        _tree_compare({**t, "pool": pool, "table": table, "lens": torch.tensor(now)}, out, lse)
+        ctx.decode_step(tok, None, tok.clone())
+    with pytest.raises(P.FirstError) as e:
+        ctx.tree_attn(desc.n_layers, d["q"], d["k"], d["v"], d["offs"], out, 5)
+    assert e.value.code == -1
+    ctx.close()
 
 
 # ---- draws ---------------------------------------------------------------------------------------------------------------
