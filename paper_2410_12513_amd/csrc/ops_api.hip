@@ -184,8 +184,11 @@ int first_op_rope(void* hip_stream, const first_rope_desc* d, const void* x, int
   P.rows = rows; P.heads = d->n_heads; P.hd = d->head_dim; P.rot = d->rot_dim; P.interleaved = d->layout == FIRST_ROPE_INTERLEAVED;
   P.amplitude = d->amplitude; P.sign = d->inverse ? -1.f : 1.f;
   const double two_pi = 6.283185307179586476925, step = -2.0 * std::log((double)d->base) / d->rot_dim;
+  double ones[8], eights[ROPE_MAX_PAIRS / 8];               // base^(-2 i / rot_dim) as a product of two: 24 exponentials at most
+  for (int i = 0; i < 8; ++i) ones[i] = std::exp(step * i);
+  for (int i = 0; 8 * i < d->rot_dim / 2; ++i) eights[i] = std::exp(step * 8 * i);
   for (int i = 0; i < d->rot_dim / 2; ++i) {
-    const double f = std::exp(step * i);
+    const double f = ones[i % 8] * eights[i / 8];
     double g = f;
     if (d->scaling == FIRST_ROPE_LINEAR) g = f / d->factor;
     if (d->scaling == FIRST_ROPE_BANDS) {

@@ -227,25 +227,32 @@ __device__ inline void sr_sort(unsigned long long* list, int n) {
       else { __builtin_amdgcn_fence(__ATOMIC_SEQ_CST, "wavefront"); __builtin_amdgcn_wave_barrier(); }
     }
 }
+// Running sum over the lanes of a wave, in the lanes themselves (rows of 16, then their last lanes handed on).
+__device__ __forceinline__ unsigned long long sr_wave_sums(unsigned long long v) {
+#define FIRST_SUM_STEP(CTRL, ROWS)                                                                                 \
+  {                                                                                                                \
+    const uint32_t lo = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(uint32_t)v, CTRL, ROWS, 0xf, false);         \
+    const uint32_t hi = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(uint32_t)(v >> 32), CTRL, ROWS, 0xf, false); \
+    v += ((unsigned long long)hi << 32) | lo;                                                                      \
+  }
+  FIRST_SUM_STEP(0x111, 0xf) FIRST_SUM_STEP(0x112, 0xf) FIRST_SUM_STEP(0x114, 0xf) FIRST_SUM_STEP(0x118, 0xf)
+  FIRST_SUM_STEP(0x142, 0xa) FIRST_SUM_STEP(0x143, 0xc)
+#undef FIRST_SUM_STEP
+  return v;
+}
 // Exclusive running sum over the threads, and the sum of all.
 __device__ __forceinline__ unsigned long long sr_scan(unsigned long long v, unsigned long long* wave, unsigned long long& all) {
-  const int tid = threadIdx.x;
-  unsigned long long incl = v;
-#pragma unroll
-  for (int d = 1; d < 64; d <<= 1) {
-    const unsigned long long o = (unsigned long long)__shfl_up((long long)incl, d, 64);
-    if ((tid & 63) >= d) incl += o;
-  }
+  const int tid = threadIdx.x, lane = tid & 63;
+  const unsigned long long incl = sr_wave_sums(v);
   __syncthreads();
-  if ((tid & 63) == 63) wave[tid >> 6] = incl;
+  if (lane == 63) wave[tid >> 6] = incl;
   __syncthreads();
-  unsigned long long base = 0;
-  all = 0;
-  for (int w = 0; w < SR_WAVES; ++w) {
-    if (w < tid >> 6) base += wave[w];
-    all += wave[w];
-  }
-  return base + incl - v;
+  static_assert(SR_WAVES == 16, "a row of lanes holds the waves' sums");
+  const unsigned long long w = sr_wave_sums(lane < SR_WAVES ? wave[lane] : 0ull);
+  const int before = __builtin_amdgcn_readfirstlane((tid >> 6) - 1);
+  auto at = [&](int l) { return ((unsigned long long)(uint32_t)__builtin_amdgcn_readlane((int)(w >> 32), l) << 32) | (uint32_t)__builtin_amdgcn_readlane((int)w, l); };
+  all = at(SR_WAVES - 1);
+  return (before >= 0 ? at(max(before, 0)) : 0ull) + incl - v;
 }
 // Whole numbers of a fraction of a mass: what a running sum has to reach (at least 1), and what it has to pass.
 __device__ __forceinline__ unsigned long long sr_reach(float p, unsigned long long total) {
