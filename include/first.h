@@ -352,7 +352,8 @@ int first_op_gemm_nt_f32a(void *hip_stream, const float *A, const void *W, float
  *   A DEV [m, k], W DEV [n, k], La DEV [n_adapters, r, k], Lb DEV [n_adapters, n, r] of dtype, on 16 bytes; adapter DEV int32 [m];
  *   scale DEV fp32 [n_adapters] (lora_alpha / r); C DEV fp32 [m, n], which none of the others may overlap; k multiple of 8; 1 <= r <= 64.
  *   m, n, k <= 2^20.  Adapters of smaller ranks: zeros in the rest of La or Lb.
- * Products of bf16 values are exact, all sums fp32; La A[i] stays in fp32 (bf16: three bf16 parts, which is all of it). */
+ * Products of bf16 values are exact, all sums fp32; La A[i] stays in fp32 (bf16: three bf16 parts, which is all of it).  Infinities and NaN in an
+ * adapter reach its own rows only, and there may be NaN where one number's product would be an infinity. */
 int64_t first_op_gemm_nt_lora_workspace(int32_t dtype, int32_t m, int32_t n, int32_t k, int32_t r);
 int first_op_gemm_nt_lora(void *hip_stream, int32_t dtype, const void *A, const void *W, const void *La, const void *Lb,
                           const int32_t *adapter, const float *scale, float *C, int32_t m, int32_t n, int32_t k, int32_t n_adapters,
@@ -404,7 +405,7 @@ typedef struct first_tree_attn_desc {
  *   node_offsets DEV int32 [B + 1], ascending, max_nodes <= 2048; of a sequence's nodes the first max_nodes are computed, rows of other nodes stay as they are
  *   tree_mask    DEV uint64 [N, mask_words], mask_words * 64 >= max_nodes (may be NULL)
  *   lse          DEV fp32 [N, n_q_heads] (may be NULL)
- * max_len <= 2^28.  N = node_offsets[B], max_nodes and max_len are bounds that the host knows; out must overlap nothing else. */
+ * B <= 65535, N <= 2^27, max_len <= 2^28.  N = node_offsets[B], max_nodes and max_len are bounds that the host knows; out must overlap nothing else. */
 int64_t first_op_tree_attn_workspace(const first_tree_attn_desc *desc, int32_t B, int32_t N, int32_t max_nodes, int32_t max_len);
 int first_op_tree_attn(void *hip_stream, const first_tree_attn_desc *desc, const void *q, const void *k_new, const void *v_new,
                        const void *kv_layer, const int32_t *page_table, const int32_t *lens, const int32_t *node_offsets,
@@ -430,7 +431,7 @@ int first_tree_attn(first_ctx *ctx, int32_t layer, const void *q, const void *k_
  * takes the first token of the order.  Logits that are NaN or -inf, and weights that are 0 in 64 bits, are no tokens; if the largest logit is +inf, the
  * tokens with +inf share the draw.  A row without tokens: token -1, logprob -inf, kept 0.  Weights in fp64, their sums exact to 2^-45 of the largest
  * weight a token (2^18 tokens), whatever the order of additions: results do not depend on the launch.
- *   logits      DEV fp32 [rows], pitch elements apart;  uniforms DEV fp32 [rows], in [0, 1) (others are taken as the nearest)
+ *   logits      DEV fp32 [rows], pitch elements apart, vocab <= 2^30;  uniforms DEV fp32 [rows], in [0, 1) (others are taken as the nearest)
  *   temperature DEV fp32 [rows] (NULL: 1);  top_k DEV int32 [rows];  top_p, min_p DEV fp32 [rows]
  *   token_out   DEV int32 [rows];  logprob_out DEV fp32 [rows] logarithm of the token's share of the kept weights (may be NULL)
  *   kept_out    DEV int32 [rows] number of tokens kept (may be NULL) */

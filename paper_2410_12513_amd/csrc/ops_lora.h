@@ -348,7 +348,7 @@ __global__ void __launch_bounds__(WGM * WGN * 64, 1) k_lora_tile(LoraArgs P) {
       auto multiply = [&](const Step& st) __attribute__((always_inline)) {
 #pragma unroll
         for (int i = 0; i < H; ++i) {
-          u32x4_t part[3];
+          u32x4_t part[3];                                 // (cut off, not rounded: 3 x 8 bits are all 24, and the largest values stay finite; an infinity is its first part)
           if constexpr (sizeof(E) == 2) {
             float x[EPC];
 #pragma unroll
@@ -357,8 +357,10 @@ __global__ void __launch_bounds__(WGM * WGN * 64, 1) k_lora_tile(LoraArgs P) {
             for (int q = 0; q < 3; ++q)
 #pragma unroll
               for (int e = 0; e < 4; ++e) {
-                part[q][e] = pk_bf16(x[2 * e], x[2 * e + 1]);
-                x[2 * e] -= __uint_as_float(part[q][e] << 16); x[2 * e + 1] -= __uint_as_float(part[q][e] & 0xffff0000u);
+                const float y = __uint_as_float(__float_as_uint(x[2 * e]) & 0xffff0000u), z = __uint_as_float(__float_as_uint(x[2 * e + 1]) & 0xffff0000u);
+                part[q][e] = __float_as_uint(y) >> 16 | __float_as_uint(z);
+                x[2 * e] = x[2 * e] == y ? 0.f : x[2 * e] - y;
+                x[2 * e + 1] = x[2 * e + 1] == z ? 0.f : x[2 * e + 1] - z;
               }
           }
           const uint32_t of = (uint32_t)(st.rows >> (32 * i)) >> (4 * lg);

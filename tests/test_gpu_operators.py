@@ -115,6 +115,25 @@ def test_lora_rows_do_not_depend_on_their_neighbours_adapters():
         assert not bool(torch.isfinite(C.cpu()[mine]).all())
 
 
+@pytest.mark.parametrize("m", [7, 60, 90, 300])
+def test_lora_first_products_at_the_end_of_the_range(m):
+    """T between the largest bf16 number and the largest fp32 one is finite; T beyond is an infinity, of its sign in every column."""
+    import paper_2410_12513_amd as P
+    A, W, La, Lb = torch.zeros((m, 64), dtype=BF), torch.ones((130, 64), dtype=BF), torch.zeros((2, 5, 64), dtype=BF), torch.ones((2, 130, 5), dtype=BF)
+    A[:, :2] = 1
+    La[:, 0, 0], La[0, 0, 1], La[1, 0, 1] = torch.finfo(BF).max, 2.0 ** 119, 2.0 ** 127
+    Lb *= 2.0 ** -20
+    Lb[:, ::3] *= -1
+    ids = (torch.arange(m) % 2).int()
+    C = torch.empty((m, 130), device="cuda")
+    P.op_gemm_nt_lora(*[t.cuda() for t in (A, W, La, Lb, ids, torch.ones(2))], C)
+    ref, size = F.lora(A, W, La, Lb, ids, torch.ones(2))
+    assert float(F.lora(A, W, La, Lb.sign(), ids, torch.ones(2))[0].abs().max()) > torch.finfo(FP).max
+    C = C.cpu().double()
+    assert bool(((C - ref).abs() <= 2e-6 * size)[ids == 0].all())
+    assert torch.equal(C[ids == 1], (ref.sign() * float("inf"))[ids == 1])
+
+
 def test_lora_merged_weights_give_the_same(dtype=FP):
     """One task for all rows: what first_lora_merge puts into the matrix."""
     import paper_2410_12513_amd as P
