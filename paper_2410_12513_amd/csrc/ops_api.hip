@@ -234,7 +234,7 @@ static int tree_refusal(const first_tree_attn_desc* d, int32_t B, int32_t N, int
   if (!std::isfinite(d->scale) || d->n_pages < 0 || d->max_pages < 0 || d->mask_words < 0)
     return refuse(FIRST_ERR_ARG, "first_op_tree_attn: scale not finite, or a negative size");
   if (B < 0 || N < 0 || max_nodes < 0 || max_len < 0) return refuse(FIRST_ERR_ARG, "first_op_tree_attn: a negative size");
-  if (B > 65535) return refuse(FIRST_ERR_CAPACITY, "first_op_tree_attn: more than 65535 sequences");
+  if (B > 65535 || N > 1 << 27) return refuse(FIRST_ERR_CAPACITY, "first_op_tree_attn: more than 65535 sequences or 2^27 nodes");
   if (max_nodes > TREE_MAX_NODES || max_len > 1 << 28) return refuse(FIRST_ERR_CAPACITY, "first_op_tree_attn: more than 2048 nodes of a sequence, or 2^28 positions");
   return FIRST_OK;
 }
@@ -276,6 +276,7 @@ int first_op_tree_attn(void* hip_stream, const first_tree_attn_desc* d, const vo
 
 int64_t first_sample_workspace(int32_t rows, int32_t vocab) {
   if (rows < 0 || vocab < 1) return refuse(FIRST_ERR_ARG, "first_sample_workspace: negative rows, or vocab < 1");
+  if (vocab > 1 << 30) return refuse(FIRST_ERR_CAPACITY, "first_sample: more than 2^30 tokens");
   return 0;
 }
 
@@ -283,6 +284,7 @@ int first_sample(void* hip_stream, const float* logits, int64_t pitch, int32_t r
                  const int32_t* top_k, const float* top_p, const float* min_p, int32_t* token_out, float* logprob_out, int32_t* kept_out, void* workspace,
                  int64_t workspace_bytes) {
   const int64_t need = first_sample_workspace(rows, vocab);
+  if (need == FIRST_ERR_CAPACITY) return FIRST_ERR_CAPACITY;
   if (need < 0 || pitch < vocab || pitch > INT32_MAX) return refuse(FIRST_ERR_ARG, "first_sample: negative rows, vocab < 1, or a pitch below vocab or above 2^31 - 1");
   if (rows == 0) return FIRST_OK;
   if (!logits || !uniforms || !token_out || (need > 0 && !workspace)) return refuse(FIRST_ERR_ARG, "first_sample: null pointer");

@@ -100,6 +100,19 @@ def test_sample_workspace(lib):
         _refused(lib, lib.first_sample(*{**args, "size": need - 1}.values()), -3, "workspace")
 
 
+def test_sizes_beyond_the_limits(lib):
+    d = B._TreeAttnDesc(**TREE_DESC)
+    assert lib.first_op_tree_attn_workspace(C.byref(d), 2, (1 << 27) + 1, 4, 1 << 20) == -3
+    _refused(lib, lib.first_op_tree_attn(None, C.byref(d), *{**TREE, "N": (1 << 27) + 1}.values()), -3, "2^27")
+    assert lib.first_sample_workspace(1, (1 << 30) + 1) == -3
+    _refused(lib, lib.first_sample(*{**SAMPLE, "vocab": (1 << 30) + 1, "pitch": (1 << 30) + 1}.values()), -3, "2^30")
+
+
+def test_tree_attention_without_a_context(lib):
+    assert lib.first_tree_attn_workspace(None, 4, 4) == -1
+    assert lib.first_tree_attn(None, 0, A16, A16, A16, A16, None, 0, A16, None, 4, 4, A16, BIG) == -1
+
+
 def test_nothing_to_do_is_no_error(lib):
     assert lib.first_op_gemm_nt_lora(*{**LORA, "m": 0, "A": 0, "C": 0, "ws": 0, "size": 0}.values()) == 0
     d = B._RopeDesc(**ROPE_DESC)
