@@ -284,8 +284,7 @@ class FirstContext:
             need = self.lib.first_tree_attn_workspace(self.h, N, max_nodes)
             if need < 0:
                 self._chk(int(need))
-            workspace = torch.empty(max(1, need), dtype=torch.uint8, device=f"cuda:{dev}")
-            workspace.record_stream(self.stream or torch.cuda.default_stream(dev))
+            workspace = _scratch(max(1, int(need)), dev, self.stream or torch.cuda.default_stream(dev))
         self._chk(self.lib.first_tree_attn(self.h, layer, *ptrs, words, *outs, N, max_nodes, workspace.data_ptr(), workspace.numel() * workspace.element_size()))
 
     def get_hidden(self) -> torch.Tensor:
@@ -423,6 +422,14 @@ def _code(t: torch.Tensor, name: str) -> int:
 _current = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda dev: torch.cuda.current_stream(dev).cuda_stream)
 
 
+def _scratch(size: int, dev: int, stream) -> torch.Tensor:
+    """Memory of that stream (None: the current one): what another stream gave back may still be in use there."""
+    if stream is None:
+        return torch.empty(size, dtype=torch.uint8, device=f"cuda:{dev}")
+    with torch.cuda.stream(stream):
+        return torch.empty(size, dtype=torch.uint8, device=f"cuda:{dev}")
+
+
 def _launch(dev: int, stream, workspace: Optional[torch.Tensor], need, call) -> None:
     """call(stream, workspace address, bytes) with device `dev` current, on `stream` or its current stream; a workspace of need() bytes lives until
     that stream is through with it, unless the caller brings one."""
@@ -440,9 +447,7 @@ def _launch(dev: int, stream, workspace: Optional[torch.Tensor], need, call) -> 
         if size < 0:
             _raise(size)
         if size > 0:
-            workspace = torch.empty(size, dtype=torch.uint8, device=f"cuda:{dev}")
-            if stream is not None:
-                workspace.record_stream(stream)
+            workspace = _scratch(size, dev, stream)
             at = workspace.data_ptr()
     rc = call(st, at, size)
     if rc != 0:

@@ -703,3 +703,23 @@ def test_results_are_the_same_bits_every_time():
         a[0](); b[0]()
         torch.cuda.synchronize()
         assert all(torch.equal(a[1][k], b[1][k]) for k in a[1])
+
+
+def test_workspaces_of_another_stream():
+    """Memory that the current stream has given back and still writes is no workspace for a call on another one."""
+    import paper_2410_12513_amd as P
+    args = [t.cuda() for t in _lora_inputs(BF, 8, 600, 512, 8, 3, seed=9)]
+    plain, C, side = torch.empty((8, 600), device="cuda"), torch.empty((8, 600), device="cuda"), torch.cuda.Stream()
+    need = P.op_gemm_nt_lora_workspace(args[0], args[1], args[2])
+    ws = torch.empty(need, dtype=torch.uint8, device="cuda")
+    P.op_gemm_nt_lora(*args, plain, workspace=ws)
+    torch.cuda.synchronize()
+    for _ in range(300):
+        ws.fill_(255)
+    at = ws.data_ptr()
+    del ws
+    from paper_2410_12513_amd import binding
+    assert binding._scratch(need, 0, side).data_ptr() != at
+    P.op_gemm_nt_lora(*args, C, stream=side)
+    side.synchronize()
+    assert torch.equal(C, plain)
