@@ -294,8 +294,9 @@ int first_sample(void* hip_stream, const float* logits, int64_t pitch, int32_t r
   if (workspace_bytes < need) return refuse(FIRST_ERR_CAPACITY, "first_sample: the workspace is smaller than first_sample_workspace says");
   int bits = 0;
   while (bits < 31 && (int64_t)1 << bits < vocab) ++bits;
-  SampleArgs P = {logits, pitch, vocab, bits, std::min(50, 62 - bits), uniforms, temperature, top_k, top_p, min_p, token_out, logprob_out, kept_out};
-  return launched("first_sample", launch<&k_sample_row>(stream_of(hip_stream), dim3(rows), SR_THREADS, 0, P));
+  const int held = std::min(SR_HELD, (vocab / 4 + SR_THREADS - 1) / SR_THREADS);
+  SampleArgs P = {logits, pitch, vocab, bits, std::min(50, 62 - bits), held, uniforms, temperature, top_k, top_p, min_p, token_out, logprob_out, kept_out};
+  return launched("first_sample", launch<&k_sample_row>(stream_of(hip_stream), dim3(rows), SR_THREADS, (size_t)held * SR_THREADS * 16, P, (size_t)SR_HELD * SR_THREADS * 16));
 }
 
 }  // extern "C"

@@ -17,6 +17,7 @@ struct SampleArgs {
   const float* logits;
   long long pitch;
   int vocab, index_bits, S;               // index_bits: of vocab - 1
+  int held;                               // pieces of a thread that LDS holds
   const float *uniforms, *temperature;    // per row; temperature, top_k, top_p, min_p may be null
   const int* top_k;
   const float *top_p, *min_p;
@@ -48,29 +49,35 @@ struct SrRow {                            // what a row's weights are made of
   // tokens that count at all: the weight is not 0 in 64 bits
   __device__ __forceinline__ bool counts(float l, double x) const { return l > -INFINITY && x > -1074.5; }
   // 2^t.  f, the rest of t to the nearest whole number: 2^f = 1 + f q(f), q of degree 9 through the Chebyshev points of [-1/2, 1/2] (6e-16)
+  // (the numbers opaque in scalar registers: seen as constants they are copied to a vector register before every step, nine more instructions)
+  __device__ __forceinline__ static double series(double f) {
+    auto k = [](double v) __attribute__((always_inline)) { asm("" : "+s"(v)); return v; };
+    double p = k(7.070977963327673e-09);
+    p = fma(p, f, k(1.0205905547945269e-07));
+    p = fma(p, f, k(1.3215451634133493e-06));
+    p = fma(p, f, k(1.5252672924230416e-05));
+    p = fma(p, f, k(0.00015403530424769424));
+    p = fma(p, f, k(0.001333355820079545));
+    p = fma(p, f, k(0.00961812910761868));
+    p = fma(p, f, k(0.05550410866465167));
+    p = fma(p, f, k(0.24022650695910075));
+    p = fma(p, f, k(0.6931471805599462));
+    return fma(p, f, 1.0);
+  }
   __device__ __forceinline__ static double power(double t) {
-    const double n = rint(t), f = t - n;
-    double p = 7.070977963327673e-09;
-    p = fma(p, f, 1.0205905547945269e-07);
-    p = fma(p, f, 1.3215451634133493e-06);
-    p = fma(p, f, 1.5252672924230416e-05);
-    p = fma(p, f, 0.00015403530424769424);
-    p = fma(p, f, 0.001333355820079545);
-    p = fma(p, f, 0.00961812910761868);
-    p = fma(p, f, 0.05550410866465167);
-    p = fma(p, f, 0.24022650695910075);
-    p = fma(p, f, 0.6931471805599462);
-    p = fma(p, f, 1.0);
-    return ldexp(p, (int)n);
+    const double n = rint(t);
+    return ldexp(series(t - n), (int)n);
   }
   // The weight times 2^S as a whole number; 0 for NaN and -inf.  (A sum with 2^52 has the whole number, rounded, in its low bits.)  The largest logit must be
   // finite here, or l is it.
   __device__ __forceinline__ unsigned long long mass(float l) const {
-    const double t = l == INFINITY ? (double)S : fma((double)l - (double)lmax, c, (double)S);
-    return (unsigned long long)__double_as_longlong(power(fmax(t, -64.0)) + 4503599627370496.0) & 0xfffffffffffffull;
+    return whole(fmax(l == INFINITY ? (double)S : fma((double)l - (double)lmax, c, (double)S), -64.0));
   }
-  __device__ __forceinline__ unsigned long long mass_finite(float l) const {
-    return (unsigned long long)__double_as_longlong(power(fmax(fma((double)l - (double)lmax, c, (double)S), -64.0)) + 4503599627370496.0) & 0xfffffffffffffull;
+  // 2^t as a whole number, t <= 50 not far below 0: f and q as above, and the sum with 2^(52 - n), n the whole part of t, leaves 2^n (1 + f q(f)) rounded in its low bits
+  __device__ __forceinline__ static unsigned long long whole(double t) {
+    const double x = 6755399441055744.0 - t, f = t + (x - 6755399441055744.0);           // (3 2^51: -n in the low bits of x)
+    const double y = series(f) + __hiloint2double((__double2loint(x) << 20) + ((1023 + 52) << 20), 0);
+    return (unsigned long long)__double_as_longlong(y) & 0xfffffffffffffull;
   }
   __device__ __forceinline__ bool heavy(double x, float min_p) const { return power(fmax(x, -1100.0)) >= (double)min_p; }
 };
@@ -167,8 +174,11 @@ struct SrFast {
 };
 union SrLds { SrShared slow; SrFast fast; };
 
-// f(logit, index) of every logit of the row, a thread's four at a time, SR_U pieces looked at while the next SR_U are on their way.
-template <typename F> __device__ __forceinline__ void sr_each(const float* row, int V, F f) {
+// The row in pieces of four logits, a thread's own ones 4 * SR_THREADS logits apart: four(piece, index of its first logit) of each, and one(logit, index) of what
+// fills no piece; SR_U pieces are looked at while the next SR_U are on their way.  FIRST: the thread's first `held` pieces go to LDS, where later looks find them.
+constexpr int SR_HELD = 7;
+struct SrHeld { float4* lds; int n; };
+template <bool FIRST, typename F, typename G> __device__ __forceinline__ void sr_each(const float* row, int V, SrHeld held, F four, G one) {
   const int pieces = V / 4, tid = threadIdx.x, mine = pieces > tid ? (pieces - tid + SR_THREADS - 1) / SR_THREADS : 0;
   SrFour a[SR_U], b[SR_U];
   auto fetch = [&](SrFour (&x)[SR_U], int i) __attribute__((always_inline)) {
@@ -178,21 +188,32 @@ template <typename F> __device__ __forceinline__ void sr_each(const float* row, 
   auto look = [&](const SrFour (&x)[SR_U], int i) __attribute__((always_inline)) {
 #pragma unroll
     for (int u = 0; u < SR_U; ++u)
-      if (i + u < mine)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) f(x[u].v[e], 4 * (tid + SR_THREADS * (i + u)) + e);
+      if (i + u < mine) {
+        if (FIRST && i + u < held.n) held.lds[(i + u) * SR_THREADS + tid] = make_float4(x[u].v[0], x[u].v[1], x[u].v[2], x[u].v[3]);
+        four(x[u], 4 * (tid + SR_THREADS * (i + u)));
+      }
   };
   const float last = tid < V - 4 * pieces ? row[4 * pieces + tid] : 0.f;
-  if (mine > 0) {
-    fetch(a, 0);
-    for (int i = 0; i < mine; i += 2 * SR_U) {
-      if (i + SR_U < mine) fetch(b, i + SR_U);
-      look(a, i);
-      if (i + 2 * SR_U < mine) fetch(a, i + 2 * SR_U);
-      if (i + SR_U < mine) look(b, i + SR_U);
+  const int i0 = FIRST ? 0 : held.n;
+  if (i0 < mine) fetch(a, i0);
+  if (!FIRST)
+    for (int u = 0; u < min(held.n, mine); ++u) {
+      const float4 x = held.lds[u * SR_THREADS + tid];
+      four(SrFour{{x.x, x.y, x.z, x.w}}, 4 * (tid + SR_THREADS * u));
     }
+  for (int i = i0; i < mine; i += 2 * SR_U) {
+    if (i + SR_U < mine) fetch(b, i + SR_U);
+    look(a, i);
+    if (i + 2 * SR_U < mine) fetch(a, i + 2 * SR_U);
+    if (i + SR_U < mine) look(b, i + SR_U);
   }
-  if (tid < V - 4 * pieces) f(last, 4 * pieces + tid);
+  if (tid < V - 4 * pieces) one(last, 4 * pieces + tid);
+}
+template <typename F> __device__ __forceinline__ void sr_each(const float* row, int V, SrHeld held, F f) {
+  sr_each<false>(row, V, held, [&](const SrFour& x, int i) __attribute__((always_inline)) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) f(x.v[e], i + e);
+  }, f);
 }
 __device__ __forceinline__ unsigned long long sr_key(float l, int i) { return (unsigned long long)sr_order(l) << 32 | (uint32_t)~i; }
 
@@ -271,12 +292,12 @@ struct SrOut { int token; float value; unsigned long long kept_mass; int kept; }
 
 // Equal parts of [lmax - range, lmax], a logit's part is (lmax - l) times this; what weighs less than 2^-66 is in the last one.
 __device__ __forceinline__ float sr_parts(const SrRow& R, float lmin) {
-  const float range = fminf(R.lmax - lmin, (float)(66.0 / R.c));
+  const float all = (float)(66.0 / R.c), range = R.lmax - lmin > 1e-30f ? fminf(R.lmax - lmin, all) : all;
   return range > 1e-30f && range < INFINITY ? (SR_PARTS - 1) / range : 0.f;
 }
-struct SrFirst { float value; int index; };                // a thread's own largest logit
+struct SrFirst { float value; int index; };                // a thread's own largest logit, and an index that is its or a little larger
 // False: the list did not fit.
-__device__ inline bool sr_fast(const float* row, int V, const SrRow& R, const SrRules& Q, SrFirst first, float lmin, SrFast& sh, SrOut& out) {
+__device__ __forceinline__ bool sr_fast(const float* row, int V, SrHeld held, const SrRow& R, const SrRules& Q, SrFirst first, float lmin, SrFast& sh, SrOut& out) {
   const int tid = threadIdx.x;
   const bool by_prefix = Q.top_k > 0 && Q.top_k <= SR_TOPK, whole = V <= 512 || (V <= SR_LIST && Q.top_k > SR_TOPK);      // (512: put in order in one go)
   const bool cut_p = !Q.greedy && Q.top_p < 1.f, cut_m = !Q.greedy && Q.min_p > 0.f;
@@ -305,8 +326,9 @@ __device__ inline bool sr_fast(const float* row, int V, const SrRow& R, const Sr
       for (int i = tid; i < V; i += SR_THREADS) sh.list[i] = row[i] > -INFINITY ? sr_key(row[i], i) : 0ull;
       if (tid == 0) sh.found = V;
     } else {
-      sr_each(row, V, [&](float l, int i) {
-        if (!(l > -INFINITY)) return;
+      const float least = bound != 0 ? sr_value((uint32_t)(bound >> 32)) : -3.402823466e38f;
+      sr_each(row, V, held, [&](float l, int i) {
+        if (!(l >= least)) return;                         // (nor NaN and -inf)
         const unsigned long long key = sr_key(l, i);
         if (key < bound) return;
         const int to = atomicAdd(&sh.found, 1);
@@ -319,13 +341,19 @@ __device__ inline bool sr_fast(const float* row, int V, const SrRow& R, const Sr
     auto part = [&](float l) __attribute__((always_inline)) { return (int)fminf((R.lmax - l) * inv, (float)(SR_PARTS - 1)); };
     for (int i = tid; i < SR_PARTS; i += SR_THREADS) sh.hist[i] = 0ull;
     __syncthreads();
-    unsigned mine = 0;
-    auto add = [&](float l, int b) __attribute__((always_inline)) {
-      const unsigned long long w = R.mass_finite(l);
-      if (w != 0) atomicAdd(&sh.hist[b], w);               // (what weighs nothing would crowd the last part)
-    };
-    sr_each(row, V, [&](float l, int) { add(l, part(l)); });
-    if (!cut_p && !cut_m) sr_each(row, V, [&](float l, int) { mine += R.counts(l, R.log2w(l)); });
+    // (what weighs nothing would crowd the last part: zeros are spread over the threads' own)
+    const float lowest = fmaxf((float)((double)R.lmax - (R.S + 2) / R.c * (1.0 + 1e-6)), -3.402823466e38f);
+    const double c = R.c, top = R.lmax, S = R.S;
+    auto mass = [&](float l) __attribute__((always_inline)) { return SrRow::whole(fmax(fma((double)l - top, c, S), -64.0)); };
+    auto bin = [&](float l) __attribute__((always_inline)) { return l >= lowest ? part(l) : tid; };
+    sr_each<false>(row, V, held, [&](const SrFour& x, int) {
+      unsigned long long w[4];
+      int to[4];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) { w[e] = mass(x.v[e]); to[e] = bin(x.v[e]); }
+#pragma unroll
+      for (int e = 0; e < 4; ++e) atomicAdd(&sh.hist[to[e]], w[e]);
+    }, [&](float l, int) { atomicAdd(&sh.hist[bin(l)], mass(l)); });
     __syncthreads();
     unsigned long long h[4], total;                        // four parts a thread: the sums through them
 #pragma unroll
@@ -372,16 +400,30 @@ __device__ inline bool sr_fast(const float* row, int V, const SrRow& R, const Sr
     at(sr_pass(Q.u, largest) + 1, [&](int i, unsigned long long) { sh.d2 = i; });
     __syncthreads();
     const int c1 = sh.c1, c2 = sh.c2, d1 = sh.d1, d2 = sh.d2;
-    unsigned ahead = 0;                                    // tokens before c1
-    sr_each(row, V, [&](float l, int i) {
+    unsigned ahead = 0;                                    // tokens before c1; without cuts, all
+    // (a part is where min((lmax - l) inv, last) ends up when cut off: in whole steps of the bounds)
+    const float fc1 = (float)c1, fc2 = (float)(c2 + 1), fd1 = (float)d1, fd2 = (float)(d2 + 1);
+    auto wanted = [&](float l) __attribute__((always_inline)) {
+      const float y = fminf((R.lmax - l) * inv, (float)(SR_PARTS - 1));
+      ahead += cut ? y < fc1 : R.counts(l, R.log2w(l));
+      return ((int)(y >= fc1) & (int)(y < fc2)) | ((int)(y >= fd1) & (int)(y < fd2));
+    };
+    auto take = [&](float l, int i) __attribute__((always_inline)) {
       if (!(l > -INFINITY)) return;
-      const int b = part(l);
-      ahead += b < c1;
-      if ((unsigned)(b - c1) > (unsigned)(c2 - c1) && (unsigned)(b - d1) > (unsigned)(d2 - d1)) return;
       const int to = atomicAdd(&sh.found, 1);
       if (to < SR_LIST) sh.list[to] = sr_key(l, i);
+    };
+    sr_each<false>(row, V, held, [&](const SrFour& x, int i) {
+      int is[4];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) is[e] = wanted(x.v[e]);
+      if (is[0] | is[1] | is[2] | is[3])
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          if (is[e]) take(x.v[e], i + e);
+    }, [&](float l, int i) {
+      if (wanted(l)) take(l, i);
     });
-    if (!cut) ahead = mine;
 #pragma unroll
     for (int d = 32; d > 0; d >>= 1) ahead += (unsigned)__shfl_xor((int)ahead, d, 64);
     if ((tid & 63) == 0) sh.count[tid >> 6] = ahead;
@@ -484,12 +526,19 @@ __device__ inline bool sr_fast(const float* row, int V, const SrRow& R, const Sr
 // grid (rows), a workgroup a row.
 __global__ void __launch_bounds__(SR_THREADS) k_sample_row(SampleArgs P) {
   __shared__ SrLds lds;
+  extern __shared__ __align__(16) char sr_smem[];
+  const SrHeld held = {reinterpret_cast<float4*>(sr_smem), P.held};
   const int tid = threadIdx.x, seq = blockIdx.x, V = P.vocab;
   const float* row = P.logits + (size_t)seq * P.pitch;
   SrFirst first = {-INFINITY, 0};
   float lmin = INFINITY;
-  sr_each(row, V, [&](float l, int i) {
-    if (l > first.value) first = {l, i};  // (not NaN)
+  // (the index: the last of its piece, which is enough for a bound; the least logit: of every fourth, what lies below it shares the last part)
+  sr_each<true>(row, V, held, [&](const SrFour& x, int i) {
+    const float top = fmaxf(fmaxf(x.v[0], x.v[1]), fmaxf(x.v[2], x.v[3]));                 // (not NaN where one is a number)
+    if (top > first.value) first = {top, i + 3};
+    lmin = fminf(lmin, x.v[0] > -INFINITY ? x.v[0] : INFINITY);
+  }, [&](float l, int i) {
+    if (l > first.value) first = {l, i};
     lmin = fminf(lmin, l > -INFINITY ? l : INFINITY);
   });
   float m = wave_max(first.value);
@@ -515,7 +564,7 @@ __global__ void __launch_bounds__(SR_THREADS) k_sample_row(SampleArgs P) {
     Q.top_p = 1.f;
   }
   SrOut out;
-  if (!sr_fast(row, V, R, Q, first, lmin, lds.fast, out)) {
+  if (!sr_fast(row, V, held, R, Q, first, lmin, lds.fast, out)) {
     __syncthreads();
     SrSum all = {0, 0}, heavy = {0, 0};
     for (int i = tid; i < V; i += SR_THREADS) {
