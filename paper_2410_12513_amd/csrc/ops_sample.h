@@ -46,8 +46,8 @@ struct SrRow {                            // what a row's weights are made of
   int S;
   // log2 of the weight of a logit that is neither NaN nor -inf
   __device__ __forceinline__ double log2w(float l) const { return l == lmax ? 0.0 : ((double)l - (double)lmax) * c; }
-  // tokens that count at all: the weight is not 0 in 64 bits
-  __device__ __forceinline__ bool counts(float l, double x) const { return l > -INFINITY && x > -1074.5; }
+  // tokens that count at all: the weight is not 0 in 64 bits (half of the smallest number, 2^-1075, is rounded to 0, more than that is not)
+  __device__ __forceinline__ bool counts(float l, double x) const { return l > -INFINITY && x > -1075.0; }
   // 2^t.  f, the rest of t to the nearest whole number: 2^f = 1 + f q(f), q of degree 9 through the Chebyshev points of [-1/2, 1/2] (6e-16)
   // (the numbers opaque in scalar registers: seen as constants they are copied to a vector register before every step, nine more instructions)
   __device__ __forceinline__ static double series(double f) {

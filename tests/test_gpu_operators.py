@@ -549,6 +549,19 @@ def test_sample_masked_logits():
         _sample_check(l, rng.random(10), 0.5, **rules)
 
 
+@pytest.mark.parametrize("vocab", [5000, 40001])
+@pytest.mark.parametrize("fourths", [[0], [1], [2, 3], [0, 1, 2]])
+def test_sample_rows_whose_fourths_differ(vocab, fourths):
+    """Grammars that mask by index: every fourth token at the top, masked, far below, or no number."""
+    rng = np.random.default_rng(vocab + fourths[0])
+    l = _logits(6, vocab, 21)
+    for f in fourths:
+        for b, v in enumerate((l[0].max(), -math.inf, math.nan, -3.4028235e38, -1e4)):
+            l[b, f::4] = np.float32(v)
+    for rules in ({}, {"top_k": 7}, {"top_p": 0.7}, {"min_p": 0.02, "top_p": 0.97}, {"temperature": 40.0, "top_p": 0.9}, {"temperature": 1e20, "min_p": 0.1}, {"temperature": 0.01}):
+        _sample_check(l, rng.random(6), 0.5, **rules)
+
+
 def test_sample_uniforms_at_the_ends():
     l = _logits(6, 900, 11)
     edge = [0.0, 1.0 - 2.0 ** -24, 1.0, 5.0, -1.0, 1e-30]
