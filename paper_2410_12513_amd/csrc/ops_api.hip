@@ -79,7 +79,7 @@ LoraPlan lora_plan(int dtype, int m, int n, int k) {
   for (int t : {256, 128, 64}) {
     const int64_t tiles = (int64_t)((m + t - 1) / t) * ((n + t - 1) / t);
     const int64_t ks = m > 65535 ? 1 : std::max<int64_t>(1, std::min<int64_t>({CUS / tiles, steps / 8, 8}));
-    const double feed = t == 256 ? 1.0 : t == 128 ? 0.75 : 0.45, rounds = (double)((tiles * ks + CUS - 1) / CUS);
+    const double feed = t == 256 ? 1.0 : t == 128 ? 0.75 : 0.38, rounds = (double)((tiles * ks + CUS - 1) / CUS);
     const double time = rounds * ((double)t * t / feed * ((steps + ks - 1) / ks) + 8 * t * t) + (ks > 1 ? 2e5 : 0);
     if (time < fastest) { fastest = time; best = {t, (int)ks}; }
   }
