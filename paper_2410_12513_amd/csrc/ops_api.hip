@@ -55,12 +55,14 @@ template <auto kernel, typename Args> hipError_t launch(hipStream_t st, dim3 gri
 }
 
 // ---- rotary positions ------------------------------------------------------------------------------------------------------
-// Four rows a workgroup where that still leaves eight workgroups a compute unit, so that their sines are formed side by side.
+// Four rows a workgroup where one row leaves threads idle and there are rows enough for every compute unit all the same; else one.  bf16, 16384 rows of heads of 128:
+// 8 heads 14.6 us by fours against 18.7, 16 heads 21.5 against 26.8, 40 heads 65.0 against 58.2; 2048 rows of 8 heads 7.2 either way.
 template <typename T> hipError_t launch_rope(hipStream_t st, const RopeArgs& P) {
   constexpr int EPC = 16 / (int)sizeof(T);
   const bool whole = (P.interleaved ? P.rot : P.rot / 2) % EPC == 0 && P.hd % EPC == 0 && P.x_pitch % EPC == 0 && P.y_pitch % EPC == 0 && aligned(P.x, 16) && aligned(P.y, 16);
   if (!whole) return launch<&k_rope<T>>(st, dim3(P.rows), WG, 0, P);
-  if (P.rows >= 4 * 8 * CUS)
+  const int items = P.rot / 2 / (P.interleaved ? EPC / 2 : EPC) + (P.hd - P.rot) / EPC;                 // threads' worth of a head
+  if (P.heads * items <= WG && P.rows >= 4 * CUS)
     return P.interleaved ? launch<&k_rope_chunks<T, true, 4>>(st, dim3((P.rows + 3) / 4), WG, 0, P) : launch<&k_rope_chunks<T, false, 4>>(st, dim3((P.rows + 3) / 4), WG, 0, P);
   return P.interleaved ? launch<&k_rope_chunks<T, true, 1>>(st, dim3(P.rows), WG, 0, P) : launch<&k_rope_chunks<T, false, 1>>(st, dim3(P.rows), WG, 0, P);
 }
