@@ -68,8 +68,11 @@ template <typename T> hipError_t launch_rope(hipStream_t st, const RopeArgs& P) 
 }
 
 // ---- projections with an adapter per row -----------------------------------------------------------------------------------
-// stream: up to 32 rows, slices of K such that two workgroups a compute unit are busy, of four steps at least.  tile: the BM x BN with the least estimated time, rounds
-// of the chip times the tile's products over how well it feeds the matrix cores; slices of K where the tiles of one round leave half of the chip idle.
+// stream: up to 32 rows, slices of K such that two workgroups a compute unit are busy, of four steps at least; up to 64 where the slices that fit A's place in LDS stay
+// few.  us a call in bf16, stream and the best tile: 16 and 32 x 4096 x 4096 16 and 21; 64 x 688 x 256 10.6 and 12.7; 64 x 14336 x 4096 46.6 and 34.5.
+// tile: the BM x BN with the least estimated time, rounds of the chip times the tile's products over how well it feeds the matrix cores; slices of K where the tiles
+// of one round leave half of the chip idle.  Tiles of 64 / 128 / 256: 33 x 4096 x 4096 20.9 / 21.9 / 29.3, 250 x 4096 x 4096 37.2 / 30.8 / 37.3 (128 without slices 52),
+// 250 x 14336 x 4096 75 / 54.6 / 62.3, 1024 x 4096 x 4096 79.7 / 62.6 / 73.1, 1024 x 14336 x 4096 231 / 194 / 137.
 struct LoraPlan { int tile, ks; };        // tile 0: stream
 LoraPlan lora_plan(int dtype, int m, int n, int k) {
   const int64_t steps = up((int64_t)k * size_of(dtype), 128) / 128;
@@ -115,7 +118,8 @@ template <typename E> hipError_t launch_lora(hipStream_t st, LoraArgs& P, const 
 
 // ---- attention of drafted tokens -------------------------------------------------------------------------------------------
 // Rows of a workgroup: the smallest block that holds a sequence's nodes times the query heads of a KV head, up to 256, as its keys are then
-// read once.  Splits: as many as fill the chip's places for workgroups once (by LDS: two a compute unit up to 80 KB, else one), of whole 128 keys (fp32: 64, whose products take the matrix cores four times as long a bit).
+// read once (rows of up to 244 over 20000 to 32768 positions in blocks of 256 168 us, of 128 176).  Splits: as many as fill the chip's places for workgroups once (by LDS: two a compute unit up to 80 KB, else one), of whole 128 keys (fp32: 64, whose products take the matrix cores four times as long a bit); twice as
+// many splits: 43.6 us against 31 for 16 sequences of 300 to 2300 positions.
 struct TreePlan { int block, split_keys, splits, row_blocks; };
 TreePlan tree_plan(const first_tree_attn_desc& d, int B, int max_nodes, int max_len) {
   const int64_t rows = (int64_t)max_nodes * (d.n_q_heads / d.n_kv_heads);

@@ -2,10 +2,14 @@
 //   T[i][p] = scale[a_i] sum_k La[a_i][p][k] A[i][k],   C[i][j] (+)= sum_k A[i][k] W[j][k] + sum_p T[i][p] Lb[a_i][j][p]
 // with a_i the adapter of row i; a_i outside [0, adapters): no second term.
 //
-// Up to 32 rows (decode steps): one pass over W, bound by its bytes.  k_lora_stream cuts W into 64 rows x a slice of K a workgroup, enough of
+// Few rows (decode steps): one pass over W, bound by its bytes.  k_lora_stream cuts W into 64 rows x a slice of K a workgroup, enough of
 // them to keep the whole chip loading, and forms T beside it; k_lora_finish adds the slices and the adapters' second products.
+//   16 x 4096 x 4096, rank 8, 16 adapters, bf16: 16 us a call (13.1 + 4.3 in a trace), 36 MB at 2.2 TB/s, floor 7.1: a launch's start and end and the join are half of it.
 // More rows: T first (k_lora_shrink), then k_lora_tile, tiles through LDS with the second product ahead of the first K step; or, where a few tiles would leave
 // the chip idle, tiles of slices of K and k_lora_finish.
+//   250 x 14336 x 4096, rank 16: 55 us (48 tiles + 10 T), floor 27; a compute unit's loads arrive at 60 bytes a ns, 470 MB of them in 128 x 128 tiles.
+//   4096 x 4096 x 14336, rank 8: 435 us (400-430 tiles + 50 T), 1.11 PFLOP/s, floor 341 at the rate of a large product; loads alone take 380: L2 delivers rows
+//   28 KB apart at half of its rate for adjacent ones.  Matrix cores are busy 63 % of the time.
 //
 // Products of bf16 values are exact in fp32, and T stays fp32: three bf16 parts in its product.  A product with an adapter is kept apart and
 // added to its own rows only, so an infinity in an adapter stays with the rows that use it.
@@ -143,10 +147,10 @@ template <typename E> __global__ void __launch_bounds__(LORA_SHRINK_WAVES * 64) 
   lora_shrink<E, LORA_SHRINK_WAVES>(P, blockIdx.x, reinterpret_cast<float*>(lora_smem));
 }
 
-// ---- up to 32 rows ---------------------------------------------------------------------------------------------------------
+// ---- few rows --------------------------------------------------------------------------------------------------------------
 // The first shrink_tiles * shrink_ways workgroups form T; the others take 64 rows of W (a wave 16) x a slice of K.  The slice of A goes into LDS once, and
-// every wave loads its rows of W straight into a ring of its own: it waits for nobody.  Two workgroups a compute unit (80 KB each), 96 KB of W in
-// flight on it.  Partial sums [slice][m][n].
+// every wave loads its rows of W straight into a ring of its own: it waits for nobody.  Two workgroups a compute unit (80 KB each), up to 80 KB of W in
+// flight on it (five of a wave's six steps).  Partial sums [slice][m][n].
 constexpr int LORA_A_BYTES = 32 * 1024;   // of LDS for the slice of A
 template <typename E, int MR, int S>      // MR: 16, 32 or 64 rows of A; S steps in a wave's ring
 __global__ void __launch_bounds__(WG, 2) k_lora_stream(LoraArgs P) {
@@ -211,7 +215,7 @@ __global__ void __launch_bounds__(WG, 2) k_lora_stream(LoraArgs P) {
   }
 }
 
-// C from the slices of K, the adapters' second products and what was there: grid (columns / 256, rows).
+// C from the slices of K, the adapters' second products and what was there: grid (columns / 256, rows).  Bound by two round trips: the row's adapter, then everything else.
 template <typename E>
 __global__ void __launch_bounds__(WG) k_lora_finish(LoraArgs P) {
   constexpr int EPC = 16 / (int)sizeof(E);
@@ -237,9 +241,11 @@ __global__ void __launch_bounds__(WG) k_lora_finish(LoraArgs P) {
 
 // ---- more rows -------------------------------------------------------------------------------------------------------------
 // BM x BN tile, WGM x WGN waves, K steps of RB bytes a row, S of them in the LDS ring; loads go straight into LDS, a row's chunks permuted against bank
-// conflicts, and the fragments of the next half chunk pair are read while the present ones are multiplied, across the barrier too.  ks > 1: partial sums of a
-// slice of K; ks = 1: the adapters' second products and the result.  Accumulators of the 32x32 MFMA: lane l holds column l % 32, register r holds
+// conflicts (none counted), and the fragments of the next 32 bytes of K are read while the present ones are multiplied, across the barrier too.  ks > 1: partial sums
+// of a slice of K; ks = 1: the adapters' second products and the result.  Accumulators of the 32x32 MFMA: lane l holds column l % 32, register r holds
 // row 8 (r / 4) + 4 (l / 32) + r % 4.
+//   256 x 256: steps of 128 bytes, two of them in LDS; of 64 bytes, four of them, half a line a load: 490 us against 437 at 4096 x 4096 x 14336.  Four waves of 128 x 128: 557.
+//   Requesting the lines of later steps into L2 ahead of time made it slower (444 -> 467; 60 -> 71 at 250 x 14336 x 4096).
 template <typename E, int BM, int BN, int WGM, int WGN, int RB, int S>
 __global__ void __launch_bounds__(WGM * WGN * 64, 1) k_lora_tile(LoraArgs P) {
   constexpr int NW = WGM * WGN, TM = BM / WGM, TN = BN / WGN, IM = TM / 32, JN = TN / 32, EPC = 16 / (int)sizeof(E);

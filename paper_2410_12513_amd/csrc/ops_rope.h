@@ -4,6 +4,9 @@
 //
 // Angles are formed in 64 bits (a position of 10^5 times a frequency of 1 has no digits to lose in 32), as turns, so that the
 // reduction is one subtraction; sine and cosine of the rest in 32.
+//
+// Bound: HBM, one read and one write of the heads; 16384 rows of 40 heads of 128 bf16 in 60 us, 5.6 TB/s.  (Pairs of elements a thread instead of chunks: 101 us.)  Small
+// calls, 64 rows, 3.8 us: a round trip for the positions, the fp64 products, a round trip for the heads.
 #pragma once
 #include "common.h"
 
@@ -31,7 +34,7 @@ __device__ __forceinline__ float2 rope_cs(const RopeArgs& P, int pos, int i) {
 
 // Rows whose heads start on 16 bytes and whose pairs fill whole chunks of 16 bytes: a workgroup takes R rows, their sines into LDS (a pair of a row a
 // thread), then chunks of their heads: two of them, half a turned part apart (half), or one (interleaved) that hold whole pairs, or one that passes.
-// ROPE_U chunks of a thread on their way at a time.  Bound: HBM; a pass is one read and one write of the heads.
+// ROPE_U chunks of a thread on their way at a time.
 constexpr int ROPE_U = 4;
 template <typename T, bool INTER, int R>
 __global__ void __launch_bounds__(WG) k_rope_chunks(RopeArgs P) {
@@ -96,7 +99,7 @@ __global__ void __launch_bounds__(WG) k_rope_chunks(RopeArgs P) {
   }
 }
 
-// Any other row: grid (rows), a workgroup a row, an element pair a thread.
+// Any other row (odd pitches and offsets, pairs that fill no chunk): grid (rows), a workgroup a row, an element pair a thread.
 template <typename T>
 __global__ void __launch_bounds__(WG) k_rope(RopeArgs P) {
   __shared__ float2 cs[ROPE_MAX_PAIRS];

@@ -8,6 +8,10 @@
 // numbers (a weight is rounded to a multiple of 2^-S, S such that a row's sum fits 62 bits): their sums do not depend on the order of
 // additions, and a token's share is off by 2^-S-1 at most, 1e-14 at 128256 tokens.  32-bit sums would put one draw in some 10^4 of a flat
 // row of that size beside its token.
+//
+// 256 rows of 128256 logits, top_p: 97 us, floor 26 (131 MB): a workgroup, so a compute unit, a row.  60 % of the time its vector units issue: some 30 instructions a logit
+// for the masses, ten for the list, four for the maximum; the rest is a row's own chain, sort and sums of the list (a fifth), which no other row fills in for.
+// One row of 32000 logits with all rules: 14 to 16 us, that chain.
 #pragma once
 #include "common.h"
 
@@ -68,8 +72,7 @@ struct SrRow {                            // what a row's weights are made of
     const double n = rint(t);
     return ldexp(series(t - n), (int)n);
   }
-  // The weight times 2^S as a whole number; 0 for NaN and -inf.  (A sum with 2^52 has the whole number, rounded, in its low bits.)  The largest logit must be
-  // finite here, or l is it.
+  // The weight times 2^S as a whole number; 0 for NaN and -inf.  The largest logit must be finite here, or l is it.
   __device__ __forceinline__ unsigned long long mass(float l) const {
     return whole(fmax(l == INFINITY ? (double)S : fma((double)l - (double)lmax, c, (double)S), -64.0));
   }
