@@ -120,7 +120,7 @@ template <typename E> hipError_t launch_lora(hipStream_t st, LoraArgs& P, const 
 // Rows of a workgroup: the smallest block that holds a sequence's nodes times the query heads of a KV head, up to 256, as its keys are then
 // read once (rows of up to 244 over 20000 to 32768 positions in blocks of 256 168 us, of 128 176).  Splits: as many as fill the chip's places for workgroups once (by LDS: two a compute unit up to 80 KB, else one), of whole 128 keys (fp32: 64, whose products take the matrix cores four times as long a bit); twice as
 // many splits: 43.6 us against 31 for 16 sequences of 300 to 2300 positions.
-struct TreePlan { int block, split_keys, splits, row_blocks; };
+struct TreePlan { int block, split_keys, splits, row_blocks, places, step; };
 TreePlan tree_plan(const first_tree_attn_desc& d, int B, int max_nodes, int max_len) {
   const int64_t rows = (int64_t)max_nodes * (d.n_q_heads / d.n_kv_heads);
   const bool wide = d.dtype == FIRST_DTYPE_BF16;
@@ -131,12 +131,21 @@ TreePlan tree_plan(const first_tree_attn_desc& d, int B, int max_nodes, int max_
   const int64_t base = std::max<int64_t>(1, (int64_t)B * d.n_kv_heads * p.row_blocks);
   const int64_t want = std::max<int64_t>(1, places / base);
   const int least = wide ? 128 : 64;
-  p.split_keys = (int)std::min<int64_t>(TREE_SPLIT_MAX, std::max<int64_t>(least, up((max_len + want - 1) / want, least)));
+  // Sequences may differ in length (2 to 64 of them): where splits of one length would be longer than the least, the kernel decides from the lengths, down to a quarter as
+  // long.  us, one length and so: one of 32768 and 15 of 300 149 and 84, 8 of 4000 to 32000 135 and 118, 4 of 32000 211 and 210, 16 of 1300 27.6 and 28.9.
+  p.step = least;
+  p.places = B > 1 && B <= 64 && want > 1 && max_len > least * want ? places / d.n_kv_heads : 0;
+  const int64_t most = p.places > 0 ? 4 * want : want;
+  p.split_keys = (int)std::min<int64_t>(TREE_SPLIT_MAX, std::max<int64_t>(least, up((max_len + most - 1) / most, least)));
   p.splits = std::max(1, (max_len + p.split_keys - 1) / p.split_keys);
+  if (p.splits == 1) p.places = 0;
   return p;
 }
 template <typename E, int HD, int QG, int KH, int NS, int S> hipError_t launch_tree_walk(hipStream_t st, const TreeArgs& P, const TreePlan& p) {
-  return launch<&k_tree_attn<E, HD, QG, KH, NS, S>>(st, dim3(P.Hkv * p.row_blocks, p.splits, P.B), QG * KH * 64, (size_t)S * 2 * KH * NS * 32 * HD * sizeof(E), P);
+  // (all splits of the greatest length have a place)
+  const int64_t least = (int64_t)P.B * p.row_blocks * ((P.max_len + TREE_SPLIT_MAX - 1) / TREE_SPLIT_MAX);
+  const dim3 grid = p.places > 0 ? dim3(P.Hkv, (unsigned)std::max<int64_t>(p.places, least), 1) : dim3(P.Hkv * p.row_blocks, p.splits, P.B);
+  return launch<&k_tree_attn<E, HD, QG, KH, NS, S>>(st, grid, QG * KH * 64, (size_t)S * 2 * KH * NS * 32 * HD * sizeof(E), P);
 }
 template <typename E, int HD> hipError_t launch_tree(hipStream_t st, const TreeArgs& P, const TreePlan& p) {
   hipError_t e;
@@ -249,7 +258,7 @@ int64_t first_op_tree_attn_workspace(const first_tree_attn_desc* d, int32_t B, i
   const int rc = tree_refusal(d, B, N, max_nodes, max_len);
   if (rc != FIRST_OK) return rc;
   const TreePlan p = tree_plan(*d, B, max_nodes, max_len);
-  return p.splits == 1 ? 0 : (int64_t)p.splits * N * d->n_q_heads * (d->head_dim + 2) * 4;
+  return p.splits == 1 ? 0 : 16 + (int64_t)p.splits * N * d->n_q_heads * (d->head_dim + 2) * 4;
 }
 
 int first_op_tree_attn(void* hip_stream, const first_tree_attn_desc* d, const void* q, const void* k_new, const void* v_new, const void* kv_layer,
@@ -268,9 +277,10 @@ int first_op_tree_attn(void* hip_stream, const first_tree_attn_desc* d, const vo
   if (workspace_bytes < need) return refuse(FIRST_ERR_CAPACITY, "first_op_tree_attn: the workspace is smaller than first_op_tree_attn_workspace says");
   const TreePlan p = tree_plan(*d, B, max_nodes, max_len);
   TreeArgs P = {q, k_new, v_new, kv_layer, page_table, lens, node_offsets, (const unsigned long long*)tree_mask, out, lse, B, N, d->n_q_heads, d->n_kv_heads, d->n_pages,
-                cached ? d->max_pages : 0, d->mask_words, max_nodes, max_len, d->scale, p.split_keys, p.splits, nullptr, nullptr};
+                cached ? d->max_pages : 0, d->mask_words, max_nodes, max_len, d->scale, p.split_keys, p.splits, p.places, p.step, p.block, nullptr, nullptr, nullptr};
   if (need > 0) {
-    P.part = (float*)workspace;
+    P.keys = (int*)workspace;
+    P.part = (float*)workspace + 4;
     P.ml = P.part + (size_t)p.splits * N * d->n_q_heads * d->head_dim;
   }
   const hipStream_t st = stream_of(hip_stream);

@@ -8,9 +8,10 @@
 // us a call (in a trace: walk + join), 32 query heads on 8 of 128 dims, bf16, and what bounds it:
 //   one node over 1000 positions        13.4 (10.4 + 3.2)  latency: offsets and lengths, keys, shares of a tile through LDS, the join
 //   16 trees of 9 to 16 over 300-2300   31 (27.6 + 4.6)    loads, 89 MB at 3.2 TB/s in the walk, floor 17.5
-//   4 trees of 33 to 61 over 20000 and more  166 (157-170 + 8.4)  matrix cores (without loads 130, loads alone 83), busy 43 % of the time: a third of the products are the weights'
+//   4 trees of 33 to 61 over 20000 and more  157 (150 + 8.4)  matrix cores (without loads 130, loads alone 83), busy 43 % of the time: a third of the products are the weights'
 //     second parts; floor 73
-// Tried and slower or no faster: one workgroup a unit with a ring of four tiles (38 us in the second case), waves' priorities, an order of products and loads by hand.
+// Tried and slower or no faster: one workgroup a unit with a ring of four tiles (38 us in the second case), waves' priorities, an order of products and loads by hand,
+// scores of the next tile formed between the exponentials of this one.
 #pragma once
 #include <type_traits>
 
@@ -26,7 +27,9 @@ struct TreeArgs {
   float* lse;
   int B, N, Hq, Hkv, n_pages, max_pages, words, max_nodes, max_len;
   float scale;
-  int split_keys, splits;                 // keys of a split, splits of max_len
+  int split_keys, splits;                 // keys of a split, at least, and splits of max_len then
+  int places, step, block;                // places > 0: the splits are as long as fills that many workgroups a KV head, a multiple of step; rows of a workgroup
+  int* keys;                              // places > 0: how long they are, for the join
   float *part, *ml;                       // splits > 1: [split][N * Hq][hd] weighted values, [split][N * Hq][2] maximum (as an exponent of 2) and sum
 };
 constexpr int TREE_PAGE = 16, TREE_SPLIT_MAX = 8192;
@@ -37,6 +40,33 @@ struct TreeSeq { int o0, n, len; };
 __device__ __forceinline__ TreeSeq tree_seq(const TreeArgs& P, int b) {
   const int o0 = max(0, min(P.offs[b], P.N)), n = min(min(P.offs[b + 1], P.N) - o0, P.max_nodes);
   return {o0, max(n, 0), (int)max(0ll, min((long long)min(P.lens[b], P.max_len), (long long)P.max_pages * TREE_PAGE))};
+}
+
+// Keys of a split, B <= 64 sequences: the shortest multiple of step, not below split_keys, with which all workgroups that have any find a place at once.
+__device__ __forceinline__ int tree_sums(int v) {          // running sum over the lanes
+#define FIRST_SUM_STEP(CTRL, ROWS) v += __builtin_amdgcn_update_dpp(0, v, CTRL, ROWS, 0xf, false);
+  FIRST_SUM_STEP(0x111, 0xf) FIRST_SUM_STEP(0x112, 0xf) FIRST_SUM_STEP(0x114, 0xf) FIRST_SUM_STEP(0x118, 0xf)
+  FIRST_SUM_STEP(0x142, 0xa) FIRST_SUM_STEP(0x143, 0xc)
+#undef FIRST_SUM_STEP
+  return v;
+}
+// Which of them the nth workgroup of a KV head takes: those that have keys come first, one behind the other, as empty ones in between leave places to nobody.
+struct TreeShare { int keys, b, split, rows; };            // b < 0: none
+__device__ __forceinline__ TreeShare tree_share(const TreeArgs& P, int nth) {
+  const int lane = threadIdx.x & 63;
+  const TreeSeq q = tree_seq(P, min(lane, P.B - 1));
+  const int blocks = lane < P.B ? (q.n * (P.Hq / P.Hkv) + P.block - 1) / P.block : 0, steps = (q.len + P.step - 1) / P.step, most = TREE_SPLIT_MAX / P.step;
+  auto sum = [&](int v) { return __builtin_amdgcn_readlane(tree_sums(v), 63); };
+  auto count = [&](int per) { return blocks * max(1, (steps + per - 1) / per); };
+  // (what fits, to begin with; in 64ths and no more than 2^24 a sequence)
+  int per = min(most, max(P.split_keys / P.step, sum((int)fminf((float)blocks * (float)steps / (float)P.places * 64.f, 16777216.f)) / 64));
+  while (per < most && sum(count(per)) > P.places) per += max(1, per / 32);
+  per = min(per, most);
+  const int mine = count(per), through = tree_sums(mine);
+  const unsigned long long past = __ballot(through > nth);
+  if (past == 0) return {per * P.step, -1, 0, 0};
+  const int b = __ffsll(past) - 1, rest = nth - (__builtin_amdgcn_readlane(through, b) - __builtin_amdgcn_readlane(mine, b)), rows = __builtin_amdgcn_readlane(blocks, b);
+  return {per * P.step, b, rest / rows, rest % rows};
 }
 
 // 16 bytes of both operands, multiplied: 8 bf16 of each half of the wave in one product of depth 16, or 4 fp32 in four of depth 2.
@@ -75,11 +105,18 @@ __global__ void __launch_bounds__(QG * KH * 64, QG == 1 ? 1 : 2) k_tree_attn(Tre
   __shared__ int pages[TREE_SPLIT_MAX / TREE_PAGE];
   const uint32_t lds0 = (uint32_t)(size_t)(__attribute__((address_space(3))) void*)tree_smem;
   const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)), lane = threadIdx.x & 63, col = lane & 31, gl = lane >> 5;
-  const int b = blockIdx.z, split = blockIdx.y, g = blockIdx.x % P.Hkv, G = P.Hq / P.Hkv;
-  const int row0 = blockIdx.x / P.Hkv * (32 * QG), k_lo = split * P.split_keys;
+  const int g = blockIdx.x % P.Hkv, G = P.Hq / P.Hkv;
+  TreeShare mine = {P.split_keys, (int)blockIdx.z, (int)blockIdx.y, (int)blockIdx.x / P.Hkv};
+  if (P.places > 0) {
+    mine = tree_share(P, blockIdx.y);
+    if ((blockIdx.x | blockIdx.y | threadIdx.x) == 0) *P.keys = mine.keys;
+    if (mine.b < 0) return;
+  }
+  const int b = mine.b, split = mine.split, keys = mine.keys;
+  const int row0 = mine.rows * (32 * QG), k_lo = split * keys;
   // the split's page ids before anybody knows how many of them count: one round trip less ahead of the first keys
   constexpr int PER = (TREE_SPLIT_MAX / TREE_PAGE + NW * 64 - 1) / (NW * 64);
-  const int last_pg = min((k_lo + P.split_keys) / TREE_PAGE, P.max_pages) - 1;
+  const int last_pg = min((k_lo + keys) / TREE_PAGE, P.max_pages) - 1;
   int ids[PER];
 #pragma unroll
   for (int i = 0; i < PER; ++i) {
@@ -87,7 +124,7 @@ __global__ void __launch_bounds__(QG * KH * 64, QG == 1 ? 1 : 2) k_tree_attn(Tre
     ids[i] = pg <= last_pg ? P.table[(size_t)b * P.max_pages + pg] : -1;
   }
   const TreeSeq q = tree_seq(P, b);
-  const int rows = q.n * G, k_hi = min(q.len, k_lo + P.split_keys);
+  const int rows = q.n * G, k_hi = min(q.len, k_lo + keys);
   if (row0 >= rows || (split > 0 && k_lo >= q.len)) return;
   const int n_tree = split == 0 ? (q.n + TK - 1) / TK : 0, n_tiles = n_tree + max(0, k_hi - k_lo + TK - 1) / TK;
   const int n_pg = max(0, k_hi - k_lo + TREE_PAGE - 1) / TREE_PAGE;
@@ -393,7 +430,7 @@ __global__ void __launch_bounds__(WG) k_tree_join(TreeArgs P) {
   const TreeSeq q = tree_seq(P, b);
   if (row >= q.n * P.Hq) return;
   const size_t orow = (size_t)q.o0 * P.Hq + row, all = (size_t)P.N * P.Hq;
-  const int ns = max(1, (q.len + P.split_keys - 1) / P.split_keys);
+  const int keys = P.places > 0 ? *P.keys : P.split_keys, ns = max(1, (q.len + keys - 1) / keys);
   float M = -INFINITY, o[DL] = {}, L = 0.f;
   for (int s0 = 0; s0 < ns; s0 += 4) {                     // four splits requested together, and joined as they come
     float2 ml[4];

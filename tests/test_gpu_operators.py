@@ -313,6 +313,26 @@ def test_tree_attention_over_long_caches(dtype, hd):
     _tree_compare(t, *_tree_run(t))
 
 
+@pytest.mark.parametrize("dtype", [BF, FP])
+@pytest.mark.parametrize("batch", [2, 64, 65])
+@pytest.mark.parametrize("hq,hkv,hd", [(5, 1, 64), (6, 2, 128)])
+def test_tree_sequences_of_very_different_lengths(dtype, batch, hq, hkv, hd):
+    rng = random.Random(batch)
+    lens, nodes = [rng.choice([0, 1, 17, 130, 260]) for _ in range(batch)], [rng.choice([0, 1, 1, 3, 14]) for _ in range(batch)]
+    lens[batch // 2], lens[-1], nodes[batch // 2], nodes[-1] = 3333, 1500, 2, 40
+    for kw in ({}, {"max_len": 2000, "max_nodes": 9}):
+        t = _tree_inputs(dtype, lens, nodes, hq, hkv, hd, seed=batch)
+        _tree_compare(t, *_tree_run(t, **kw), **kw)
+
+
+def test_tree_more_splits_of_the_largest_size_than_places():
+    """Two sequences whose splits of 8192 keys are more than the chip takes at once; all of their pages are the same few."""
+    t = _tree_inputs(BF, [0, 0], [1, 2], 32, 32, 64, seed=8)
+    g = torch.Generator().manual_seed(8)
+    t["pool"], t["table"], t["lens"] = _randn(g, (64, 2, 32, 16, 64), BF), torch.randint(0, 64, (2, 4375), generator=g).int(), torch.tensor([70000, 69003], dtype=torch.int32)
+    _tree_compare(t, *_tree_run(t))
+
+
 def test_tree_splits_of_the_largest_size():
     """So many heads that a sequence is cut into splits of the largest size only; the others are short."""
     t = _tree_inputs(BF, [8300, 0, 3, 17, 5, 1, 40, 16], [1, 1, 2, 1, 0, 1, 1, 1], 64, 64, 64, seed=12)
