@@ -89,7 +89,8 @@ template <typename E, int RB> __device__ __forceinline__ int tree_vslot(int row,
 typedef short tree_s4_t __attribute__((ext_vector_type(4)));
 typedef __attribute__((address_space(3))) tree_s4_t* tree_lds4_t;
 
-// QG groups of 32 rows x KH shares of a tile's keys (NS blocks of 32 each); S tiles in the ring.  grid (KV heads x blocks of 32 QG rows, splits, B)
+// QG groups of 32 rows x KH shares of a tile's keys (NS blocks of 32 each); S tiles in the ring.  grid (KV heads x blocks of 32 QG rows, splits, B);
+// with places: (KV heads, places), what a workgroup takes by tree_share
 //
 // Everything is transposed, so that a lane owns ONE row of the result (column of the products): S^T = K Q^T and O^T = V^T P^T with the weights
 // straight from the accumulators of S^T, bf16 ones split into two parts (with one part their rounding would be as large as that of the
